@@ -39,7 +39,7 @@ enum {
     VBR_EUNSUPPORTED = -5  /* valid input the GPU path does not take (see vbr_upload) */
 };
 
-enum { VBR_F16 = 0, VBR_BF16 = 1 };
+enum { VBR_F16 = 0, VBR_BF16 = 1, VBR_F32 = 2 };   /* VBR_F32: where a call names it, no type of a sparse matrix */
 
 /*
  * Sparse matrix in CSR (section 2), borrowed from the caller, host memory.
@@ -268,6 +268,107 @@ enum {
 };
 int vbr_probe_launch(int32_t kind, void *buf_dev, int64_t buf_bytes, int32_t iters, void *hip_stream,
                      double *work);
+
+/*
+ * Routed products.  Where the path above groups the rows of a matrix once, on the host, by the columns they touch, a layer
+ * of experts groups its rows at every call, on the device, by the matrix a router chose for them; the rows of one matrix are again one
+ * dense product.  The calls in turn:
+ *
+ *   route_topk      raw scores [n_rows][n_experts] -> the ids and weights of top_k experts for every row
+ *   route_plan      ids -> the (row, place) pairs of every expert together
+ *   q4_mm_routed    each pair's row times its expert's matrix, which is kept in 4 bits
+ *   route_combine   the sum of a row's results by its weights
+ *
+ * with route_topk_grad and route_combine_grad for training a router, and q4_mm for rows that all meet one matrix.  All of
+ * them are asynchronous on hip_stream, allocate nothing, copy nothing to the host and can be captured into a graph; every size is known
+ * on the host, what the ids say only on the device.  Calls on distinct outputs (and plans) may run at the same time on any streams of the device
+ * the operands are on, which has to be the current one.  Operands must not overlap outputs.  Results do not depend on what else runs: nothing is
+ * added atomically, and sums are taken in a fixed order.
+ *
+ * A pair is a row and one of its top_k places: pair p = row * top_k + place.  An id outside [0, n_experts) means that the pair has no
+ * expert: it is left out of the plan, its row of Y stays as it is, and it counts as nothing in the sum and its gradients.
+ */
+enum { VBR_SOFTMAX = 0, VBR_SIGMOID = 1 };
+typedef struct vbr_route {
+    int32_t n_experts;        /* 1 .. 1024 */
+    int32_t top_k;            /* 1 .. 64, at most n_experts */
+    int32_t score;            /* VBR_SOFTMAX over a row's experts, or VBR_SIGMOID of each */
+    int32_t n_groups;         /* 1 .. 64, a divisor of n_experts: groups of consecutive experts (1: no groups) */
+    int32_t top_groups;       /* 1 .. n_groups, with top_k experts at least in so many groups */
+    int32_t renormalise;      /* weights are divided by their sum */
+    float scale;              /* and multiplied by this; finite */
+} vbr_route_t;
+
+/*
+ * The choice.  score_e = softmax or sigmoid of the raw scores (in fp32, bf16 or fp16, leading dimension ld >= n_experts, in elements); an
+ * expert's key is score_e + bias_e with a bias (fp32 [n_experts]; NULL: none), which only the choice sees, and its raw score without.  With
+ * groups, the top_groups groups with the largest sums of their two best score_e (+ bias_e) stay, the others' experts are out.  The top_k
+ * largest keys win, in falling order, of equal ones the lower index; sums with a bias or within a group are compared in 64 bits.
+ *   ids [n_rows][top_k]      int32; -1 where fewer experts are open
+ *   weights [n_rows][top_k]  scale * score_e, renormalised: divided by the sum of the chosen scores; 0 where the id is -1
+ * A raw score of -inf or NaN closes the expert for its row (also in the softmax), a bias of -inf or NaN for every row; a row may have none open.
+ * +inf counts as the largest finite fp32 number.  Chosen scores that are too low for fp32 still give finite weights when renormalised.
+ */
+int route_topk(const vbr_route_t *how, const void *logits_dev, int64_t ld, int32_t logits_type, const float *bias_dev,
+               int64_t n_rows, int32_t *ids_dev, float *weights_dev, void *hip_stream);
+
+/*
+ * The gradient of the weights to the raw scores, for the ids given, the choice held fixed (no gradient reaches the bias): all of
+ * dlogits [n_rows][n_experts] (the type of the raw scores, leading dimension ldd) is written, zeros included.  An id given twice counts twice, one
+ * outside [0, n_experts) or of a closed expert not at all.
+ */
+int route_topk_grad(const vbr_route_t *how, const void *logits_dev, int64_t ld, int32_t logits_type, const int32_t *ids_dev,
+                    const float *dweights_dev, int64_t n_rows, void *dlogits_dev, int64_t ldd, void *hip_stream);
+
+/*
+ * The grouping of n_pairs pairs (at most 2^30) by their ids, into plan_dev (caller-allocated, route_plan_bytes bytes, 256-byte
+ * aligned), which q4_mm_routed reads and a caller may:
+ *   int32 offsets [n_experts + 1] at its start     pairs of expert e are order[offsets[e]] .. order[offsets[e + 1] - 1]
+ *   int32 order [n_pairs] at byte route_plan_order  pair numbers, rising inside an expert; -1 behind the last pair with an expert
+ * and behind them what the products need to know.  The whole plan is written anew by every call.  Both size functions return 0 for sizes out of range.
+ */
+int64_t route_plan_bytes(int64_t n_pairs, int32_t n_experts);
+int64_t route_plan_order(int64_t n_pairs, int32_t n_experts);
+int route_plan(const int32_t *ids_dev, int64_t n_pairs, int32_t n_experts, void *plan_dev, void *hip_stream);
+
+/*
+ * out[row] = sum over its places, in their order, of weights[pair] * y[pair]: y [n_rows * top_k][n_cols], out [n_rows][n_cols], both fp32, bf16 or
+ * fp16, sums in fp32; n_cols % 8 == 0, leading dimensions multiples of 8, 16-byte aligned.  Pairs whose id is outside [0, n_experts) are skipped
+ * (their rows of y are not read); a row without others is zeros.  The gradients: dy[pair] = weights[pair] * dout[row] in y's type and dweights[pair] = dout[row] . y[pair],
+ * both zero for skipped pairs.
+ */
+int route_combine(const void *y_dev, int64_t ldy, int32_t y_type, const int32_t *ids_dev, const float *weights_dev, int64_t n_rows,
+                  int32_t top_k, int32_t n_experts, int64_t n_cols, void *out_dev, int64_t ldo, int32_t out_type, void *hip_stream);
+int route_combine_grad(const void *dout_dev, int64_t ldo, int32_t out_type, const void *y_dev, int64_t ldy, int32_t y_type,
+                       const int32_t *ids_dev, const float *weights_dev, int64_t n_rows, int32_t top_k, int32_t n_experts, int64_t n_cols,
+                       void *dy_dev, int64_t lddy, float *dweights_dev, void *hip_stream);
+
+/*
+ * Matrices in 4 bits: n_mats of n_rows x n_cols, W[n][k] = scale[n][k / group] * (code[n][k] - zero[n][k / group]), code and zero 0 .. 15.
+ * n_cols % 32 == 0; group 32, 64 or a multiple of 128 (the last group of a row may be short).  dtype is the type of the scales and of the rows
+ * they are multiplied with.  zeros = 0: the zero point is 8 everywhere.  gated: the first half of a matrix's rows gates the second,
+ *   Y[r][n] = silu(x . W[n]) * (x . W[n + n_rows / 2]),  silu(u) = u / (1 + exp(-u)),
+ * and Y has n_rows / 2 columns instead of n_rows.
+ *   q4_upload   lays the matrices out in buf_dev (device memory of the current device, caller-allocated, q4_device_bytes bytes, 256-byte
+ *               aligned) from device arrays, each without gaps:
+ *                 codes  [n_mats][n_rows][n_cols / 2] bytes, column 2 j in the low and 2 j + 1 in the high half of byte j; 4-byte aligned
+ *                 scales [n_mats][n_rows][ceil(n_cols / group)] of dtype;  zeros the same, one byte each (not read without zeros)
+ *               on hip_stream, and waits (so it cannot be captured).  The handle keeps buf_dev, which must outlive every product; the arrays are free.
+ *   q4_mm       Y[r] = X[r] W^T for n_rows rows (n_mats must be 1)
+ *   q4_mm_routed  Y[pair] = X[row] W[expert]^T for every pair of a plan made by route_plan for n_mats experts and n_pairs pairs.  X has n_rows rows,
+ *               of which n_pairs must be a multiple: pair p meets row p / (n_pairs / n_rows) (n_pairs rows: a row for each pair).
+ * X: dtype, ldx >= n_cols, ldx % 8 == 0, 16-byte aligned.  Y: fp32 (VBR_F32) or dtype, any ldy >= its columns.  Weights are not rounded: codes are multiplied as
+ * they are on the matrix units, and scales and zero points applied to sums, in fp32; with y_type = dtype a result is rounded once.  A NaN or Inf
+ * in a row of X stays in that row's results.
+ */
+typedef struct q4 q4_t;
+int q4_create(int64_t n_mats, int64_t n_rows, int64_t n_cols, int32_t group, int32_t dtype, int32_t zeros, int32_t gated, q4_t **out);
+int64_t q4_device_bytes(const q4_t *h);
+int q4_upload(q4_t *h, const void *codes_dev, const void *scales_dev, const void *zeros_dev, void *buf_dev, void *hip_stream);
+int q4_mm(const q4_t *h, const void *X_dev, int64_t ldx, void *Y_dev, int64_t ldy, int32_t y_type, int64_t n_rows, void *hip_stream);
+int q4_mm_routed(const q4_t *h, const void *plan_dev, int64_t n_pairs, const void *X_dev, int64_t ldx, int64_t n_rows,
+                 void *Y_dev, int64_t ldy, int32_t y_type, void *hip_stream);
+void q4_free(q4_t *h);
 
 const char *vbr_strerror(int code);
 int vbr_last_hip_error(void);   /* hipError_t of the last failing HIP call on this thread */

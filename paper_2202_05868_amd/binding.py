@@ -27,7 +27,8 @@ EXPORTS = ("sa1_reorder", "vbr_build", "vbr_get_index", "vbr_unpack_block", "vbr
            "vbr_upload", "vbr_spmm", "vbr_get_schedule", "vbr_free", "vbr_strerror",
            "vbr_last_hip_error", "sa1_blocking_curve", "csr_spmm_create", "csr_device_bytes", "csr_upload",
            "csr_spmm", "csr_free", "vbr_probe_launch", "vbr_get_launches", "vbr_audit", "vbr_get_tile_ksteps",
-           "vbr_get_launch_functions")
+           "vbr_get_launch_functions", "route_topk", "route_topk_grad", "route_plan_bytes", "route_plan_order", "route_plan",
+           "route_combine", "route_combine_grad", "q4_create", "q4_device_bytes", "q4_upload", "q4_mm", "q4_mm_routed", "q4_free")
 
 
 class VbrError(RuntimeError):
@@ -37,6 +38,11 @@ class VbrError(RuntimeError):
         if code == -3:
             msg += " (hipError %d)" % _lib.vbr_last_hip_error()
         super().__init__("%s: %s" % (what, msg))
+
+
+class _Route(ctypes.Structure):
+    _fields_ = [("n_experts", ctypes.c_int32), ("top_k", ctypes.c_int32), ("score", ctypes.c_int32), ("n_groups", ctypes.c_int32),
+                ("top_groups", ctypes.c_int32), ("renormalise", ctypes.c_int32), ("scale", ctypes.c_float)]
 
 
 class _Csr(ctypes.Structure):
@@ -84,6 +90,23 @@ def _load():
     lib.csr_free.restype = None
     lib.vbr_probe_launch.argtypes = [i32, vp, i64, i32, vp, P(dbl)]
     lib.vbr_probe_launch.restype = ctypes.c_int
+    lib.route_topk.argtypes = [P(_Route), vp, i64, i32, vp, i64, vp, vp, vp]
+    lib.route_topk_grad.argtypes = [P(_Route), vp, i64, i32, vp, vp, i64, vp, i64, vp]
+    lib.route_plan_bytes.argtypes = lib.route_plan_order.argtypes = [i64, i32]
+    lib.route_plan_bytes.restype = lib.route_plan_order.restype = i64
+    lib.route_plan.argtypes = [vp, i64, i32, vp, vp]
+    lib.route_combine.argtypes = [vp, i64, i32, vp, vp, i64, i32, i32, i64, vp, i64, i32, vp]
+    lib.route_combine_grad.argtypes = [vp, i64, i32, vp, i64, i32, vp, vp, i64, i32, i32, i64, vp, i64, vp, vp]
+    lib.q4_create.argtypes = [i64, i64, i64, i32, i32, i32, i32, P(vp)]
+    lib.q4_device_bytes.argtypes = [vp]
+    lib.q4_device_bytes.restype = i64
+    lib.q4_upload.argtypes = [vp, vp, vp, vp, vp, vp]
+    lib.q4_mm.argtypes = [vp, vp, i64, vp, i64, i32, i64, vp]
+    lib.q4_mm_routed.argtypes = [vp, vp, i64, vp, i64, i64, vp, i64, i32, vp]
+    lib.q4_free.argtypes = [vp]
+    lib.q4_free.restype = None
+    for name in ("route_topk", "route_topk_grad", "route_plan", "route_combine", "route_combine_grad", "q4_create", "q4_upload", "q4_mm", "q4_mm_routed"):
+        getattr(lib, name).restype = ctypes.c_int
     for name in ("sa1_reorder", "vbr_build", "vbr_get_index", "vbr_unpack_block", "vbr_upload",
                  "vbr_spmm", "vbr_get_schedule", "sa1_blocking_curve", "csr_spmm_create", "csr_upload", "csr_spmm"):
         getattr(lib, name).restype = ctypes.c_int

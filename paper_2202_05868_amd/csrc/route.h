@@ -1,0 +1,25 @@
+// The layout of a plan (route_plan), which the routed products read.
+#pragma once
+
+#include <cstdint>
+
+#include "vbr_spmm.h"
+
+namespace vbrk {
+
+constexpr int32_t kMaxExperts = 1024;              // one thread of a workgroup each, in the scan
+constexpr int32_t kMaxTopK = 64, kMaxGroups = 64;  // one lane each
+constexpr int64_t kMaxPairs = 1 << 30;             // positions are 32 bits
+constexpr int32_t kPlanChunk = 1024;               // pairs a wave counts
+
+// Byte offsets in a plan: int32 offsets [n_experts + 1] at 0, int32 order [n_pairs], int2 tiles [n_tiles] (expert or -1, first position),
+// int32 counts [n_chunks][n_experts].
+struct PlanParts {
+    int64_t order, tiles, counts, total;
+    int64_t n_tiles, n_chunks;
+    int32_t tile_rows;
+};
+PlanParts plan_parts(int64_t n_pairs, int32_t n_experts);
+bool plan_sizes_ok(int64_t n_pairs, int32_t n_experts);
+
+}  // namespace vbrk
