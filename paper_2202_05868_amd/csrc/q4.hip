@@ -9,6 +9,7 @@
 
 #include <cstdint>
 #include <new>
+#include <type_traits>
 
 #include "route.h"
 #include "vbr_device.h"
@@ -16,7 +17,8 @@
 
 // A tile is 16 rows (of one half, if gated) and 128 columns: 1 KiB of codes, 16 bytes a lane.  Lane 16 q + n has row n; its word i has the
 // columns 32 i + 8 q .. + 7, in the order that the rotations take them apart.  Tiles of a row follow each other; with a gate the tiles of 16
-// gate rows stand before those of the 16 rows they gate.  Scales and zero points are [tile row][group][16 rows].
+// gate rows stand before those of the 16 rows they gate.  Scales and zero points are [tile row][step][16 rows][groups of a step], a step being a tile's
+// 128 columns, or a group where that is longer: one load each a lane and step.
 struct q4 {
     int64_t n_mats = 0, n_rows = 0, n_cols = 0;
     int32_t group = 0, dtype = 0;
@@ -25,10 +27,12 @@ struct q4 {
     int64_t tile_rows() const { return (rows() + 15) / 16 * (gated ? 2 : 1); }      // of a matrix
     int64_t k_tiles() const { return (n_cols + 127) / 128; }
     int64_t groups() const { return (n_cols + group - 1) / group; }
-    int64_t groups_kept() const { return (k_tiles() * 128 + group - 1) / group; }   // up to the end of the last tile
+    int32_t groups_a_step() const { return group < 128 ? 128 / group : 1; }
+    int64_t steps() const { return group < 128 ? k_tiles() : groups(); }
+    int64_t kept() const { return n_mats * tile_rows() * steps() * 16 * groups_a_step(); }
     int64_t scales_at() const { return n_mats * tile_rows() * k_tiles() * 1024; }
-    int64_t zeros_at() const { return scales_at() + n_mats * tile_rows() * groups_kept() * 32; }
-    int64_t total() const { return (zeros_at() + (zeros ? n_mats * tile_rows() * groups_kept() * 16 : 0) + 255) / 256 * 256; }
+    int64_t zeros_at() const { return scales_at() + 2 * kept(); }
+    int64_t total() const { return (zeros_at() + (zeros ? kept() : 0) + 255) / 256 * 256; }
     void *dev = nullptr;
 };
 
@@ -43,8 +47,8 @@ struct PackParams {
     uint16_t *kept_scales;
     uint8_t *kept_zeros;
     int64_t n_words, n_kept;
-    int64_t n_rows, half, n_cols, tile_rows, k_tiles, groups, groups_kept;
-    int32_t gated, rotate;
+    int64_t n_rows, half, n_cols, tile_rows, k_tiles, groups, steps;
+    int32_t gated, rotate, groups_a_step;
 };
 
 __device__ __forceinline__ int64_t source_row(const PackParams &p, int64_t tile_row, int n)       // in its matrix; -1: none
@@ -73,32 +77,32 @@ __global__ void __launch_bounds__(256) q4_pack_scales_kernel(const PackParams p)
 {
     const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (at >= p.n_kept) return;
-    const int n = at & 15;
-    const int64_t g = (at >> 4) % p.groups_kept, row_of_all = (at >> 4) / p.groups_kept, mat = row_of_all / p.tile_rows;
+    const int in_step = (int)(at % p.groups_a_step);
+    const int64_t of_step = at / p.groups_a_step;
+    const int n = of_step & 15;
+    const int64_t g = (of_step >> 4) % p.steps * p.groups_a_step + in_step, row_of_all = (of_step >> 4) / p.steps, mat = row_of_all / p.tile_rows;
     const int64_t row = source_row(p, row_of_all - mat * p.tile_rows, n), from = (mat * p.n_rows + row) * p.groups + g;
     const bool there = row >= 0 && g < p.groups;
     p.kept_scales[at] = there ? p.scales[from] : 0;
     if (p.kept_zeros) p.kept_zeros[at] = there ? p.zeros[from] : 0;
 }
 
-// ---- the product
+// ---- the products
 struct MmParams {
     const uint4v *tiles;
-    const uint16_t *scales;
-    const uint8_t *zeros;
+    const char *scales, *zeros;
     const uint16_t *X;
     void *Y;
     int64_t ldx, ldy, n_rows;                  // rows of Y
-    int64_t k_tiles, tile_rows, groups_kept;
-    int32_t half, n_cols, k_chunks, tiles_a_group;     // k_chunks: columns / 32; tiles_a_group: group / 128, at least 1
-    // routed
+    int64_t k_tiles, tile_rows, steps;
+    int32_t half, k_chunks, tiles_a_step;      // k_chunks: columns / 32
+    int32_t gated, f32;
+    int32_t col_blocks, row_tiles;             // of the launch; row_tiles: at most so many, if routed
+    // routed, or null
     const int2 *plan_tiles;
     const int32_t *offsets, *order;
     int32_t divide;                            // pairs of a row of X
 };
-
-constexpr int kMmWaves = 4;
-constexpr int kTokens = 16;
 
 template <int DT>
 __device__ __forceinline__ float as_f32(uint16_t x)
@@ -118,51 +122,95 @@ __device__ __forceinline__ short8v sixteen_plus(uint32_t w)
     return __builtin_bit_cast(short8v, r);
 }
 
+// the scales and zero points of a lane's row of W for one step: N groups
+template <int N>
+struct Words {
+    using Scales = std::conditional_t<N == 1, uint16_t, std::conditional_t<N == 2, uint32_t, uint64_t>>;
+    using Zeros = std::conditional_t<N == 1, uint8_t, std::conditional_t<N == 2, uint16_t, uint32_t>>;
+    Scales s;
+    Zeros z;
+    template <int DT>
+    __device__ __forceinline__ float scale(int i) const { return as_f32<DT>((uint16_t)(s >> (N > 1 ? 16 * i : 0))); }
+    __device__ __forceinline__ float minus_sixteen_plus_zero(int i) const { return -16.f - (float)(uint8_t)(z >> (N > 1 ? 8 * i : 0)); }
+};
+template <int N, bool ZEROS>
+__device__ __forceinline__ Words<N> load_words(const MmParams &p, int64_t row, int64_t step, int n)
+{
+    const int64_t at = (row * p.steps + step) * 16 + n;
+    Words<N> w{};
+    w.s = reinterpret_cast<const typename Words<N>::Scales *>(p.scales)[at];
+    if constexpr (ZEROS) w.z = reinterpret_cast<const typename Words<N>::Zeros *>(p.zeros)[at];
+    return w;
+}
+
 __device__ __forceinline__ float silu(float x) { return x / (1.f + expf(-x)); }
 
-// One workgroup: 16 rows of X (of one matrix) times two rows of tiles, four waves that share the columns.  The sums of the waves are added in their order.
-// CH: steps of 32 columns between applications of a scale (1, 2, or 4)
-template <int DT, int CH, bool ZEROS, bool GATED, bool ROUTED, bool F32>
-__global__ void __launch_bounds__(64 * kMmWaves) q4_mm_kernel(const MmParams p)
+template <int DT>
+__device__ __forceinline__ void store_y(const MmParams &p, int64_t at, float y)
 {
-    __shared__ float sums[kMmWaves][2][kTokens][17];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, q = lane >> 4;
-    int64_t first = (int64_t)blockIdx.y * kTokens, mat = 0;
-    int count;
-    if constexpr (ROUTED) {
-        const int2 tile = p.plan_tiles[blockIdx.y];
-        if (tile.x < 0) return;
-        mat = tile.x;
-        first = tile.y;
-        const int left = p.offsets[tile.x + 1] - tile.y;
-        count = left < kTokens ? left : kTokens;
+    if (p.f32) static_cast<float *>(p.Y)[at] = y;
+    else if constexpr (DT == VBR_F16) static_cast<_Float16 *>(p.Y)[at] = (_Float16)y;
+    else static_cast<__bf16 *>(p.Y)[at] = (__bf16)y;
+}
+
+// rows first .. first + count - 1 (positions of the plan's order, if routed) of matrix mat
+struct RowTile {
+    int64_t mat, first;
+    int32_t count;
+};
+__device__ __forceinline__ bool row_tile(const MmParams &p, int tile, int rows, RowTile &r)
+{
+    if (p.order) {
+        const int2 t = p.plan_tiles[tile];
+        if (t.x < 0) return false;
+        const int left = p.offsets[t.x + 1] - t.y;
+        r = {t.x, t.y, left < rows ? left : rows};
     } else {
-        count = p.n_rows - first < kTokens ? (int)(p.n_rows - first) : kTokens;
+        const int64_t first = (int64_t)tile * rows, left = p.n_rows - first;
+        r = {0, first, (int32_t)(left < rows ? left : rows)};
     }
-    const int64_t last = p.tile_rows - 1, r0 = 2 * (int64_t)blockIdx.x, r1 = r0 < last ? r0 + 1 : r0;
-    const int64_t row[2] = {mat * p.tile_rows + r0, mat * p.tile_rows + r1};
-    int64_t x_row = 0;
-    if (n < count) x_row = ROUTED ? p.order[first + n] / p.divide : first + n;
-    const uint16_t *x = p.X + x_row * p.ldx + 8 * q;
+    return true;
+}
+__device__ __forceinline__ int64_t x_row(const MmParams &p, int64_t at) { return p.order ? p.order[at] / p.divide : at; }
+__device__ __forceinline__ int64_t y_row(const MmParams &p, int64_t at) { return p.order ? p.order[at] : at; }
+
+// ---- few rows: 16 of them times two rows of tiles, by four waves that share the columns.  The sums of the waves are added in their order.
+// CH: steps of 32 columns between applications of a scale (1, 2, or 4)
+constexpr int kFewWaves = 4;
+
+template <int DT, int CH, bool ZEROS>
+__global__ void __launch_bounds__(64 * kFewWaves) q4_few_kernel(const MmParams p)
+{
+    __shared__ float sums[kFewWaves][2][16][17];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, q = lane >> 4;
+    RowTile rt;
+    if (!row_tile(p, blockIdx.x / p.col_blocks, 16, rt)) return;
+    const int col_block = blockIdx.x % p.col_blocks;
+    const int64_t last = p.tile_rows - 1, r0 = 2 * (int64_t)col_block, r1 = r0 < last ? r0 + 1 : r0;
+    const int64_t row[2] = {rt.mat * p.tile_rows + r0, rt.mat * p.tile_rows + r1};
+    const uint16_t *x = p.X + (n < rt.count ? x_row(p, rt.first + n) : 0) * p.ldx + 8 * q;
 
     float4v acc[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
     const float4v none = {0, 0, 0, 0};
     const short one = DT == VBR_F16 ? 0x3C00 : 0x3F80;
     const short8v ones = {one, one, one, one, one, one, one, one};
-    const int begin = (int)(p.k_tiles * wave / kMmWaves), end = (int)(p.k_tiles * (wave + 1) / kMmWaves);
+    const int begin = (int)(p.k_tiles * wave / kFewWaves), end = (int)(p.k_tiles * (wave + 1) / kFewWaves);
     for (int t = begin; t < end; ++t) {
         uint4v w[2];
+        Words<4 / CH> sz[2];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) w[h] = p.tiles[(row[h] * p.k_tiles + t) * 64 + lane];
+        for (int h = 0; h < 2; ++h) {
+            w[h] = p.tiles[(row[h] * p.k_tiles + t) * 64 + lane];
+            sz[h] = load_words<4 / CH, ZEROS>(p, row[h], t / p.tiles_a_step, n);
+        }
         short8v xf[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             xf[i] = short8v{0, 0, 0, 0, 0, 0, 0, 0};
-            if (n < count && 4 * t + i < p.k_chunks) xf[i] = *reinterpret_cast<const short8v *>(x + 128 * (int64_t)t + 32 * i);
+            if (n < rt.count && 4 * t + i < p.k_chunks) xf[i] = *reinterpret_cast<const short8v *>(x + 128 * (int64_t)t + 32 * i);
         }
 #pragma unroll
         for (int c = 0; c < 4; c += CH) {
-            const int64_t g = CH < 4 ? (int64_t)t * (4 / CH) + c / CH : t / p.tiles_a_group;
             float4v of_x = none, part[2] = {none, none};
 #pragma unroll
             for (int i = c; i < c + CH; ++i) {
@@ -172,10 +220,9 @@ __global__ void __launch_bounds__(64 * kMmWaves) q4_mm_kernel(const MmParams p)
             }
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const int64_t at = (row[h] * p.groups_kept + g) * 16 + n;
-                const float s = as_f32<DT>(p.scales[at]), z = ZEROS ? 16.f + (float)p.zeros[at] : 24.f;
+                const float s = sz[h].template scale<DT>(c / CH), z = ZEROS ? sz[h].minus_sixteen_plus_zero(c / CH) : -24.f;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) acc[h][i] = __builtin_fmaf(s, __builtin_fmaf(-z, of_x[i], part[h][i]), acc[h][i]);
+                for (int i = 0; i < 4; ++i) acc[h][i] = __builtin_fmaf(s, __builtin_fmaf(z, of_x[i], part[h][i]), acc[h][i]);
             }
         }
     }
@@ -184,43 +231,171 @@ __global__ void __launch_bounds__(64 * kMmWaves) q4_mm_kernel(const MmParams p)
 #pragma unroll
         for (int i = 0; i < 4; ++i) sums[wave][h][4 * q + i][n] = acc[h][i];
     __syncthreads();
-    constexpr int kOut = GATED ? 1 : 2;
-    for (int at = threadIdx.x; at < kOut * 16 * kTokens; at += 64 * kMmWaves) {
-        const int col = at & 15, h = GATED ? 0 : at >> 4 & 1, token = at / (16 * kOut);
-        const int64_t out_col = (GATED ? blockIdx.x : r0 + h) * 16 + col;
-        if (token >= count || out_col >= p.half || (!GATED && r0 + h > last)) continue;
-        float v[2];
+    const int outs = p.gated ? 1 : 2;
+    for (int at = threadIdx.x; at < outs * 256; at += 64 * kFewWaves) {
+        const int col = at & 15, token = at >> 4 & 15, h = at >> 8;
+        const int64_t out_col = (p.gated ? col_block : r0 + h) * 16 + col;
+        if (token >= rt.count || out_col >= p.half || (!p.gated && r0 + h > last)) continue;
+        float v = 0.f;
 #pragma unroll
-        for (int u = 0; u < (GATED ? 2 : 1); ++u) {
-            v[u] = 0;
-            for (int k = 0; k < kMmWaves; ++k) v[u] += sums[k][GATED ? u : h][token][col];
+        for (int k = 0; k < kFewWaves; ++k) v += sums[k][h][token][col];
+        if (p.gated) {
+            float u = 0.f;
+#pragma unroll
+            for (int k = 0; k < kFewWaves; ++k) u += sums[k][1][token][col];
+            v = silu(v) * u;
         }
-        const float y = GATED ? silu(v[0]) * v[1] : v[0];
-        const int64_t y_row = ROUTED ? p.order[first + token] : first + token;
-        if constexpr (F32) static_cast<float *>(p.Y)[y_row * p.ldy + out_col] = y;
-        else if constexpr (DT == VBR_F16) static_cast<_Float16 *>(p.Y)[y_row * p.ldy + out_col] = (_Float16)y;
-        else static_cast<__bf16 *>(p.Y)[y_row * p.ldy + out_col] = (__bf16)y;
+        store_y<DT>(p, y_row(p, rt.first + token) * p.ldy + out_col, v);
     }
 }
 
+// ---- many rows: 16 MT of them times 16 rows of tiles, by four waves with four rows of tiles each.  A step is a tile's 128 columns: X goes through LDS,
+// which all waves read; W comes straight into registers, as it was laid out, and is turned into numbers there.
+constexpr int kManyRows = 4;           // rows of tiles a wave
+
+template <int CTRL>
+__device__ __forceinline__ float add_lane(float x)
+{
+    return x + __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
+}
+
+template <int DT>
+__device__ __forceinline__ float sum_of_8(uint4v x)
+{
+    float s[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) s[j] = as_f32<DT>((uint16_t)x[j]) + as_f32<DT>((uint16_t)(x[j] >> 16));
+    return (s[0] + s[1]) + (s[2] + s[3]);
+}
+
+template <int DT, int CH, bool ZEROS, int MT>
+__global__ void __launch_bounds__(256, 2) q4_many_kernel(const MmParams p)
+{
+    constexpr int kRows = 16 * MT, kGroups = 4 / CH, NT = kManyRows;
+    __shared__ __attribute__((aligned(16))) uint4v x_lds[2][kRows * 16];         // chunk c of row r at r * 16 + (c ^ r % 16)
+    __shared__ __attribute__((aligned(16))) float sum_lds[2][kGroups][kRows];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, q = lane >> 4;
+    RowTile rt;
+    if (!row_tile(p, blockIdx.x / p.col_blocks, kRows, rt)) return;
+    const int64_t last = p.tile_rows - 1, r0 = ((int64_t)(blockIdx.x % p.col_blocks) * 4 + wave) * NT;
+    int64_t row[NT];
+#pragma unroll
+    for (int h = 0; h < NT; ++h) row[h] = rt.mat * p.tile_rows + (r0 + h < last ? r0 + h : last);
+
+    // this thread's chunks of X: chunk c of rows xr + 16 j
+    const int c = threadIdx.x & 15, xr = threadIdx.x >> 4;
+    const uint16_t *src[MT];
+#pragma unroll
+    for (int j = 0; j < MT; ++j) src[j] = p.X + x_row(p, rt.first + (xr + 16 * j < rt.count ? xr + 16 * j : 0)) * p.ldx + 8 * c;
+    uint4v xv[MT], w[NT];
+    Words<kGroups> sz[NT];
+    auto fetch_x = [&](int t) {
+#pragma unroll
+        for (int j = 0; j < MT; ++j) {
+            xv[j] = uint4v{0, 0, 0, 0};
+            if (4 * t + (c >> 2) < p.k_chunks) xv[j] = *reinterpret_cast<const uint4v *>(src[j] + 128 * (int64_t)t);
+        }
+    };
+    auto put_x = [&](int buf) {
+#pragma unroll
+        for (int j = 0; j < MT; ++j) {
+            x_lds[buf][(xr + 16 * j) * 16 + (c ^ (xr & 15))] = xv[j];
+            float s = sum_of_8<DT>(xv[j]);
+            s = add_lane<0x4E>(add_lane<0xB1>(s));            // over four lanes, then eight, then sixteen
+            if constexpr (CH >= 2) s = add_lane<0x141>(s);
+            if constexpr (CH == 4) s = add_lane<0x140>(s);
+            if (c % (4 * CH) == 0) sum_lds[buf][c / (4 * CH)][xr + 16 * j] = ZEROS ? s : -24.f * s;
+        }
+    };
+    auto fetch_w = [&](int h, int t) {
+        w[h] = p.tiles[(row[h] * p.k_tiles + t) * 64 + lane];
+        sz[h] = load_words<kGroups, ZEROS>(p, row[h], t / p.tiles_a_step, n);
+    };
+    float4v acc[MT][NT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int h = 0; h < NT; ++h) acc[m][h] = float4v{0, 0, 0, 0};
+    const int n_tiles = (int)p.k_tiles;
+    fetch_x(0);
+#pragma unroll
+    for (int h = 0; h < NT; ++h) fetch_w(h, 0);
+    put_x(0);
+    __syncthreads();
+    for (int t = 0; t < n_tiles; ++t) {
+        const int buf = t & 1, next = t + 1 < n_tiles ? t + 1 : t;
+        fetch_x(next);
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) {
+            short8v xf[MT][CH];
+            float4v of_x[MT];
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+#pragma unroll
+                for (int i = 0; i < CH; ++i) xf[m][i] = __builtin_bit_cast(short8v, x_lds[buf][(16 * m + n) * 16 + ((4 * (g * CH + i) + q) ^ n)]);
+                of_x[m] = *reinterpret_cast<const float4v *>(&sum_lds[buf][g][16 * m + 4 * q]);
+            }
+#pragma unroll
+            for (int h = 0; h < NT; ++h) {
+                float4v part[MT];
+#pragma unroll
+                for (int m = 0; m < MT; ++m) {
+                    part[m] = of_x[m];
+                    if constexpr (ZEROS) part[m] *= sz[h].minus_sixteen_plus_zero(g);
+                }
+#pragma unroll
+                for (int i = 0; i < CH; ++i) {
+                    const short8v b = sixteen_plus<DT>(w[h][g * CH + i]);
+#pragma unroll
+                    for (int m = 0; m < MT; ++m) part[m] = mfma16x16x32<DT>(xf[m][i], b, part[m]);
+                }
+                const float s = sz[h].template scale<DT>(g);
+                if (g == kGroups - 1) fetch_w(h, next);      // a step ahead, into the registers just read
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[m][h][i] = __builtin_fmaf(s, part[m][i], acc[m][h][i]);
+            }
+            __builtin_amdgcn_sched_barrier(0);                // (groups taken up at once take registers that are not there)
+        }
+        if (t + 1 < n_tiles) put_x(buf ^ 1);
+        __syncthreads();
+    }
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int token = 16 * m + 4 * q + i;
+            if (token >= rt.count) continue;
+            const int64_t at = y_row(p, rt.first + token) * p.ldy;
+            if (p.gated) {
+#pragma unroll
+                for (int h = 0; h < NT; h += 2) {
+                    const int64_t col = (r0 + h) / 2 * 16 + n;
+                    if (r0 + h < last && col < p.half) store_y<DT>(p, at + col, silu(acc[m][h][i]) * acc[m][h + 1][i]);
+                }
+            } else {
+#pragma unroll
+                for (int h = 0; h < NT; ++h) {
+                    const int64_t col = (r0 + h) * 16 + n;
+                    if (col < p.half) store_y<DT>(p, at + col, acc[m][h][i]);
+                }
+            }
+        }
+}
+
 using MmKernel = void (*)(MmParams);
-template <int DT, int CH, bool ZEROS, bool GATED>
-MmKernel mm_kernel(bool routed, bool f32)
+template <int DT, int CH, bool ZEROS>
+MmKernel mm_kernel(int32_t rows)
 {
-    return routed ? (f32 ? q4_mm_kernel<DT, CH, ZEROS, GATED, true, true> : q4_mm_kernel<DT, CH, ZEROS, GATED, true, false>)
-                  : (f32 ? q4_mm_kernel<DT, CH, ZEROS, GATED, false, true> : q4_mm_kernel<DT, CH, ZEROS, GATED, false, false>);
+    return rows == 16 ? q4_few_kernel<DT, CH, ZEROS> : rows == 32 ? q4_many_kernel<DT, CH, ZEROS, 2> : q4_many_kernel<DT, CH, ZEROS, 4>;
 }
-template <int DT, int CH>
-MmKernel mm_kernel(bool zeros, bool gated, bool routed, bool f32)
+template <int DT>
+MmKernel mm_kernel(int32_t group, bool zeros, int32_t rows)
 {
-    return zeros ? (gated ? mm_kernel<DT, CH, true, true>(routed, f32) : mm_kernel<DT, CH, true, false>(routed, f32))
-                 : (gated ? mm_kernel<DT, CH, false, true>(routed, f32) : mm_kernel<DT, CH, false, false>(routed, f32));
-}
-MmKernel mm_kernel(int32_t dtype, int32_t group, bool zeros, bool gated, bool routed, bool f32)
-{
-    if (dtype == VBR_F16)
-        return group == 32 ? mm_kernel<VBR_F16, 1>(zeros, gated, routed, f32) : group == 64 ? mm_kernel<VBR_F16, 2>(zeros, gated, routed, f32) : mm_kernel<VBR_F16, 4>(zeros, gated, routed, f32);
-    return group == 32 ? mm_kernel<VBR_BF16, 1>(zeros, gated, routed, f32) : group == 64 ? mm_kernel<VBR_BF16, 2>(zeros, gated, routed, f32) : mm_kernel<VBR_BF16, 4>(zeros, gated, routed, f32);
+    if (group == 32) return zeros ? mm_kernel<DT, 1, true>(rows) : mm_kernel<DT, 1, false>(rows);
+    if (group == 64) return zeros ? mm_kernel<DT, 2, true>(rows) : mm_kernel<DT, 2, false>(rows);
+    return zeros ? mm_kernel<DT, 4, true>(rows) : mm_kernel<DT, 4, false>(rows);
 }
 
 bool aligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
@@ -250,8 +425,8 @@ MmParams mm_params(const q4_t *h, const void *X_dev, int64_t ldx, void *Y_dev, i
     MmParams p{};
     const char *d = static_cast<const char *>(h->dev);
     p.tiles = reinterpret_cast<const uint4v *>(d);
-    p.scales = reinterpret_cast<const uint16_t *>(d + h->scales_at());
-    p.zeros = reinterpret_cast<const uint8_t *>(d + h->zeros_at());
+    p.scales = d + h->scales_at();
+    p.zeros = d + h->zeros_at();
     p.X = static_cast<const uint16_t *>(X_dev);
     p.Y = Y_dev;
     p.ldx = ldx;
@@ -259,12 +434,23 @@ MmParams mm_params(const q4_t *h, const void *X_dev, int64_t ldx, void *Y_dev, i
     p.n_rows = n_rows;
     p.k_tiles = h->k_tiles();
     p.tile_rows = h->tile_rows();
-    p.groups_kept = h->groups_kept();
+    p.steps = h->steps();
     p.half = (int32_t)h->rows();
-    p.n_cols = (int32_t)h->n_cols;
     p.k_chunks = (int32_t)(h->n_cols / 32);
-    p.tiles_a_group = h->group < 128 ? 1 : h->group / 128;
+    p.tiles_a_step = h->group < 128 ? 1 : h->group / 128;
+    p.gated = h->gated;
     return p;
+}
+
+int launch_mm(const q4 *h, MmParams &p, int32_t rows, int64_t row_tiles, void *hip_stream)
+{
+    const int64_t block = rows == 16 ? 2 : 4 * kManyRows;      // rows of tiles of a workgroup
+    p.col_blocks = (int32_t)((p.tile_rows + block - 1) / block);
+    const int64_t grid = row_tiles * p.col_blocks;
+    if (grid > INT32_MAX) return VBR_EUNSUPPORTED;
+    const MmKernel kernel = h->dtype == VBR_F16 ? mm_kernel<VBR_F16>(h->group, h->zeros, rows) : mm_kernel<VBR_BF16>(h->group, h->zeros, rows);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(256), 0, static_cast<hipStream_t>(hip_stream), p);
+    return launched();
 }
 
 }  // namespace
@@ -307,14 +493,15 @@ extern "C" int q4_upload(q4_t *h, const void *codes_dev, const void *scales_dev,
     p.kept_scales = reinterpret_cast<uint16_t *>(d + h->scales_at());
     p.kept_zeros = h->zeros ? reinterpret_cast<uint8_t *>(d + h->zeros_at()) : nullptr;
     p.n_words = h->scales_at() / 4;
-    p.n_kept = h->n_mats * h->tile_rows() * h->groups_kept() * 16;
+    p.n_kept = h->kept();
     p.n_rows = h->n_rows;
     p.half = h->rows();
     p.n_cols = h->n_cols;
     p.tile_rows = h->tile_rows();
     p.k_tiles = h->k_tiles();
     p.groups = h->groups();
-    p.groups_kept = h->groups_kept();
+    p.steps = h->steps();
+    p.groups_a_step = h->groups_a_step();
     p.gated = h->gated;
     p.rotate = h->dtype == VBR_F16 ? 6 : 3;
     if ((p.n_words + 255) / 256 > INT32_MAX) return VBR_EUNSUPPORTED;
@@ -338,11 +525,10 @@ extern "C" int q4_mm(const q4_t *h, const void *X_dev, int64_t ldx, void *Y_dev,
     if (rc != VBR_OK) return rc;
     if (h->n_mats != 1) return VBR_EINVAL;
     if (n_rows == 0) return VBR_OK;
-    const MmParams p = mm_params(h, X_dev, ldx, Y_dev, ldy, n_rows);
-    const int64_t y = (n_rows + kTokens - 1) / kTokens, x = (p.tile_rows + 1) / 2;
-    if (y > 65535) return VBR_EUNSUPPORTED;
-    hipLaunchKernelGGL(mm_kernel(h->dtype, h->group, h->zeros, h->gated, false, y_type == VBR_F32), dim3((unsigned)x, (unsigned)y), dim3(64 * kMmWaves), 0, static_cast<hipStream_t>(hip_stream), p);
-    return launched();
+    MmParams p = mm_params(h, X_dev, ldx, Y_dev, ldy, n_rows);
+    p.f32 = y_type == VBR_F32;
+    const int32_t rows = n_rows <= 16 ? 16 : n_rows <= 32 ? 32 : 64;
+    return launch_mm(h, p, rows, (n_rows + rows - 1) / rows, hip_stream);
 }
 
 extern "C" int q4_mm_routed(const q4_t *h, const void *plan_dev, int64_t n_pairs, const void *X_dev, int64_t ldx, int64_t n_rows, void *Y_dev, int64_t ldy, int32_t y_type, void *hip_stream)
@@ -359,10 +545,8 @@ extern "C" int q4_mm_routed(const q4_t *h, const void *plan_dev, int64_t n_pairs
     p.order = reinterpret_cast<const int32_t *>(d + parts.order);
     p.plan_tiles = reinterpret_cast<const int2 *>(d + parts.tiles);
     p.divide = (int32_t)(n_pairs / n_rows);
-    const int64_t x = (p.tile_rows + 1) / 2;
-    if (parts.n_tiles > 65535) return VBR_EUNSUPPORTED;
-    hipLaunchKernelGGL(mm_kernel(h->dtype, h->group, h->zeros, h->gated, true, y_type == VBR_F32), dim3((unsigned)x, (unsigned)parts.n_tiles), dim3(64 * kMmWaves), 0, static_cast<hipStream_t>(hip_stream), p);
-    return launched();
+    p.f32 = y_type == VBR_F32;
+    return launch_mm(h, p, parts.tile_rows, parts.n_tiles, hip_stream);
 }
 
 extern "C" void q4_free(q4_t *h) { delete h; }

@@ -529,7 +529,12 @@ int64_t up(int64_t x, int64_t q) { return (x + q - 1) / q * q; }
 
 }  // namespace
 
-int32_t plan_tile_rows(int64_t, int32_t) { return 16; }
+// Rows of a tile of the products: by how many pairs an expert has if all have alike.
+int32_t plan_tile_rows(int64_t n_pairs, int32_t n_experts)
+{
+    const int64_t rows = n_pairs / n_experts;
+    return rows <= 12 ? 16 : rows <= 32 ? 32 : 64;
+}
 
 // Tiles of tile_rows rows that any ids can need: an expert with c > 0 pairs has at most 1 + (c - 1) / tile_rows.
 int64_t plan_max_tiles(int64_t n_pairs, int32_t n_experts, int32_t tile_rows)
