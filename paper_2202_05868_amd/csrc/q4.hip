@@ -116,9 +116,12 @@ template <int DT>
 __device__ __forceinline__ short8v sixteen_plus(uint32_t w)
 {
     constexpr uint32_t mask = DT == VBR_F16 ? 0x03C003C0u : 0x00780078u, base = DT == VBR_F16 ? 0x4C004C00u : 0x41804180u;
+    uint32_t in_scalar = mask, in_vector = base;         // one instruction takes one of each, and no constants of this size
+    asm volatile("" : "+s"(in_scalar));
+    asm volatile("" : "+v"(in_vector));
     uint4v r;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) r[j] = ((j ? __builtin_amdgcn_alignbit(w, w, 4 * j) : w) & mask) | base;
+    for (int j = 0; j < 4; ++j) r[j] = ((j ? __builtin_amdgcn_alignbit(w, w, 4 * j) : w) & in_scalar) | in_vector;
     return __builtin_bit_cast(short8v, r);
 }
 
@@ -259,28 +262,45 @@ __device__ __forceinline__ float add_lane(float x)
     return x + __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
 }
 
+typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2v __attribute__((ext_vector_type(2)));
+
 template <int DT>
 __device__ __forceinline__ float sum_of_8(uint4v x)
 {
-    float s[4];
+    float s = 0.f;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) s[j] = as_f32<DT>((uint16_t)x[j]) + as_f32<DT>((uint16_t)(x[j] >> 16));
-    return (s[0] + s[1]) + (s[2] + s[3]);
+    for (int j = 0; j < 4; ++j) {
+        const uint32_t two = x[j];                           // (a bit cast of x[j] itself takes x[0])
+        if constexpr (DT == VBR_F16) s = __builtin_amdgcn_fdot2(__builtin_bit_cast(half2v, two), half2v{1, 1}, s, false);
+        else s = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2v, two), bf16x2v{1, 1}, s, false);
+    }
+    return s;
 }
 
+// What (16 + z) takes from a sum is a product itself, of the sums of x in a group and s (16 + z): four groups at a time it goes to the matrix units in
+// fp32, so that the vector units have one multiplication and addition a sum and group.
 template <int DT, int CH, bool ZEROS, int MT>
 __global__ void __launch_bounds__(256, 2) q4_many_kernel(const MmParams p)
 {
     constexpr int kRows = 16 * MT, kGroups = 4 / CH, NT = kManyRows;
     __shared__ __attribute__((aligned(16))) uint4v x_lds[2][kRows * 16];         // chunk c of row r at r * 16 + (c ^ r % 16)
-    __shared__ __attribute__((aligned(16))) float sum_lds[2][kGroups][kRows];
+    __shared__ float sum_lds[2][4][kRows];                                       // of four groups in turn
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, q = lane >> 4;
     RowTile rt;
     if (!row_tile(p, blockIdx.x / p.col_blocks, kRows, rt)) return;
     const int64_t last = p.tile_rows - 1, r0 = ((int64_t)(blockIdx.x % p.col_blocks) * 4 + wave) * NT;
-    int64_t row[NT];
+    // W from the wave's first row of tiles on (behind the last one, that one), 32-bit offsets from there
+    const int64_t from = rt.mat * p.tile_rows + (r0 < last ? r0 : last);
+    const int further = (int)(last - r0 < 0 ? 0 : last - r0 < NT ? last - r0 : NT - 1);
+    const char *w_at = reinterpret_cast<const char *>(p.tiles) + from * p.k_tiles * 1024;
+    const char *s_at = p.scales + from * p.steps * (32 * kGroups), *z_at = p.zeros + from * p.steps * (16 * kGroups);
+    uint32_t w_row[NT], s_row[NT];
 #pragma unroll
-    for (int h = 0; h < NT; ++h) row[h] = rt.mat * p.tile_rows + (r0 + h < last ? r0 + h : last);
+    for (int h = 0; h < NT; ++h) {
+        w_row[h] = (uint32_t)((h < further ? h : further) * p.k_tiles) * 1024u;
+        s_row[h] = (uint32_t)((h < further ? h : further) * p.steps) * 16u;
+    }
 
     // this thread's chunks of X: chunk c of rows xr + 16 j
     const int c = threadIdx.x & 15, xr = threadIdx.x >> 4;
@@ -296,26 +316,32 @@ __global__ void __launch_bounds__(256, 2) q4_many_kernel(const MmParams p)
             if (4 * t + (c >> 2) < p.k_chunks) xv[j] = *reinterpret_cast<const uint4v *>(src[j] + 128 * (int64_t)t);
         }
     };
-    auto put_x = [&](int buf) {
+    auto put_x = [&](int t) {
 #pragma unroll
         for (int j = 0; j < MT; ++j) {
-            x_lds[buf][(xr + 16 * j) * 16 + (c ^ (xr & 15))] = xv[j];
+            x_lds[t & 1][(xr + 16 * j) * 16 + (c ^ (xr & 15))] = xv[j];
             float s = sum_of_8<DT>(xv[j]);
             s = add_lane<0x4E>(add_lane<0xB1>(s));            // over four lanes, then eight, then sixteen
             if constexpr (CH >= 2) s = add_lane<0x141>(s);
             if constexpr (CH == 4) s = add_lane<0x140>(s);
-            if (c % (4 * CH) == 0) sum_lds[buf][c / (4 * CH)][xr + 16 * j] = ZEROS ? s : -24.f * s;
+            const int g = t * kGroups + c / (4 * CH);
+            if (c % (4 * CH) == 0) sum_lds[g >> 2 & 1][g & 3][xr + 16 * j] = s;
         }
     };
     auto fetch_w = [&](int h, int t) {
-        w[h] = p.tiles[(row[h] * p.k_tiles + t) * 64 + lane];
-        sz[h] = load_words<kGroups, ZEROS>(p, row[h], t / p.tiles_a_step, n);
+        w[h] = *reinterpret_cast<const uint4v *>(w_at + (w_row[h] + (uint32_t)t * 1024u + (uint32_t)lane * 16u));
+        const uint32_t at = s_row[h] + (uint32_t)(t / p.tiles_a_step) * 16u + (uint32_t)n;
+        sz[h].s = *reinterpret_cast<const typename Words<kGroups>::Scales *>(s_at + at * (2u * kGroups));
+        if constexpr (ZEROS) sz[h].z = *reinterpret_cast<const typename Words<kGroups>::Zeros *>(z_at + at * (uint32_t)kGroups);
     };
     float4v acc[MT][NT];
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int h = 0; h < NT; ++h) acc[m][h] = float4v{0, 0, 0, 0};
+    float taken[NT];                                              // -s (16 + z) of the q-th of four groups
+#pragma unroll
+    for (int h = 0; h < NT; ++h) taken[h] = 0.f;
     const int n_tiles = (int)p.k_tiles;
     fetch_x(0);
 #pragma unroll
@@ -323,26 +349,21 @@ __global__ void __launch_bounds__(256, 2) q4_many_kernel(const MmParams p)
     put_x(0);
     __syncthreads();
     for (int t = 0; t < n_tiles; ++t) {
-        const int buf = t & 1, next = t + 1 < n_tiles ? t + 1 : t;
+        const int next = t + 1 < n_tiles ? t + 1 : t;
         fetch_x(next);
 #pragma unroll
         for (int g = 0; g < kGroups; ++g) {
+            const int slot = (t * kGroups + g) & 3;
             short8v xf[MT][CH];
-            float4v of_x[MT];
 #pragma unroll
-            for (int m = 0; m < MT; ++m) {
+            for (int m = 0; m < MT; ++m)
 #pragma unroll
-                for (int i = 0; i < CH; ++i) xf[m][i] = __builtin_bit_cast(short8v, x_lds[buf][(16 * m + n) * 16 + ((4 * (g * CH + i) + q) ^ n)]);
-                of_x[m] = *reinterpret_cast<const float4v *>(&sum_lds[buf][g][16 * m + 4 * q]);
-            }
+                for (int i = 0; i < CH; ++i) xf[m][i] = __builtin_bit_cast(short8v, x_lds[t & 1][(16 * m + n) * 16 + ((4 * (g * CH + i) + q) ^ n)]);
 #pragma unroll
             for (int h = 0; h < NT; ++h) {
                 float4v part[MT];
 #pragma unroll
-                for (int m = 0; m < MT; ++m) {
-                    part[m] = of_x[m];
-                    if constexpr (ZEROS) part[m] *= sz[h].minus_sixteen_plus_zero(g);
-                }
+                for (int m = 0; m < MT; ++m) part[m] = float4v{0, 0, 0, 0};
 #pragma unroll
                 for (int i = 0; i < CH; ++i) {
                     const short8v b = sixteen_plus<DT>(w[h][g * CH + i]);
@@ -350,15 +371,27 @@ __global__ void __launch_bounds__(256, 2) q4_many_kernel(const MmParams p)
                     for (int m = 0; m < MT; ++m) part[m] = mfma16x16x32<DT>(xf[m][i], b, part[m]);
                 }
                 const float s = sz[h].template scale<DT>(g);
-                if (g == kGroups - 1) fetch_w(h, next);      // a step ahead, into the registers just read
+                taken[h] = q == slot ? s * (ZEROS ? sz[h].minus_sixteen_plus_zero(g) : -24.f) : taken[h];
+                if (g == kGroups - 1) fetch_w(h, next);           // a step ahead, into the registers just read
 #pragma unroll
                 for (int m = 0; m < MT; ++m)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) acc[m][h][i] = __builtin_fmaf(s, part[m][i], acc[m][h][i]);
             }
-            __builtin_amdgcn_sched_barrier(0);                // (groups taken up at once take registers that are not there)
+            if (g == kGroups - 1 && (slot == 3 || t + 1 == n_tiles)) {
+                const int four = (t * kGroups + g) >> 2 & 1;
+#pragma unroll
+                for (int m = 0; m < MT; ++m) {
+                    const float of_x = q <= slot ? sum_lds[four][q][16 * m + n] : 0.f;
+#pragma unroll
+                    for (int h = 0; h < NT; ++h) acc[m][h] = __builtin_amdgcn_mfma_f32_16x16x4f32(of_x, taken[h], acc[m][h], 0, 0, 0);
+                }
+#pragma unroll
+                for (int h = 0; h < NT; ++h) taken[h] = 0.f;
+            }
+            __builtin_amdgcn_sched_barrier(0);                    // (groups taken up at once take registers that are not there)
         }
-        if (t + 1 < n_tiles) put_x(buf ^ 1);
+        if (t + 1 < n_tiles) put_x(t + 1);
         __syncthreads();
     }
 #pragma unroll
