@@ -99,9 +99,10 @@ struct MmParams {
     int32_t gated, f32;
     int32_t col_blocks, row_tiles;             // of the launch; row_tiles: at most so many, if routed
     // routed, or null
-    const int2 *plan_tiles;
-    const int32_t *offsets, *order;
-    int32_t divide;                            // pairs of a row of X
+    const PlanTile *plan_tiles;
+    const int32_t *order;
+    uint32_t divide;                           // the row of X of pair i is i divide >> divide_shift
+    int32_t divide_shift;
 };
 
 template <int DT>
@@ -111,19 +112,24 @@ __device__ __forceinline__ float as_f32(uint16_t x)
     else return __builtin_bit_cast(float, (uint32_t)x << 16);
 }
 
-// eight numbers 16 + c out of a word
+// Eight numbers 16 + c out of a word.  One instruction takes a constant of this size from a scalar register and one from a vector register, and
+// none from its own code: they are kept in registers.
 template <int DT>
-__device__ __forceinline__ short8v sixteen_plus(uint32_t w)
-{
-    constexpr uint32_t mask = DT == VBR_F16 ? 0x03C003C0u : 0x00780078u, base = DT == VBR_F16 ? 0x4C004C00u : 0x41804180u;
-    uint32_t in_scalar = mask, in_vector = base;         // one instruction takes one of each, and no constants of this size
-    asm volatile("" : "+s"(in_scalar));
-    asm volatile("" : "+v"(in_vector));
-    uint4v r;
+struct SixteenPlus {
+    uint32_t mask = DT == VBR_F16 ? 0x03C003C0u : 0x00780078u, base = DT == VBR_F16 ? 0x4C004C00u : 0x41804180u;
+    __device__ __forceinline__ SixteenPlus()
+    {
+        asm volatile("" : "+s"(mask));
+        asm volatile("" : "+v"(base));
+    }
+    __device__ __forceinline__ short8v operator()(uint32_t w) const
+    {
+        uint4v r;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) r[j] = ((j ? __builtin_amdgcn_alignbit(w, w, 4 * j) : w) & in_scalar) | in_vector;
-    return __builtin_bit_cast(short8v, r);
-}
+        for (int j = 0; j < 4; ++j) r[j] = ((j ? __builtin_amdgcn_alignbit(w, w, 4 * j) : w) & mask) | base;
+        return __builtin_bit_cast(short8v, r);
+    }
+};
 
 // the scales and zero points of a lane's row of W for one step: N groups
 template <int N>
@@ -146,7 +152,14 @@ __device__ __forceinline__ Words<N> load_words(const MmParams &p, int64_t row, i
     return w;
 }
 
-__device__ __forceinline__ float silu(float x) { return x / (1.f + expf(-x)); }
+// x / (1 + exp(-x)).  exp(-x) is 2^t (1 + r), r what rounding took from t = -x log2(e): a relative error of a few steps however large x is.
+__device__ __forceinline__ float silu(float x)
+{
+    constexpr float log2e = 1.44269502f, rest = 1.92596299e-8f, ln2 = 0.693147181f;      // log2(e) in two numbers
+    const float t = -x * log2e, r = __builtin_fmaf(-x, rest, __builtin_fmaf(-x, log2e, -t));
+    const float e = __builtin_amdgcn_exp2f(t);
+    return x * __builtin_amdgcn_rcpf(1.f + __builtin_fmaf(e, r * ln2, e));
+}
 
 template <int DT>
 __device__ __forceinline__ void store_y(const MmParams &p, int64_t at, float y)
@@ -161,20 +174,16 @@ struct RowTile {
     int64_t mat, first;
     int32_t count;
 };
-__device__ __forceinline__ bool row_tile(const MmParams &p, int tile, int rows, RowTile &r)
+__device__ __forceinline__ RowTile row_tile(const MmParams &p, int tile, int rows)      // count 0: none
 {
     if (p.order) {
-        const int2 t = p.plan_tiles[tile];
-        if (t.x < 0) return false;
-        const int left = p.offsets[t.x + 1] - t.y;
-        r = {t.x, t.y, left < rows ? left : rows};
-    } else {
-        const int64_t first = (int64_t)tile * rows, left = p.n_rows - first;
-        r = {0, first, (int32_t)(left < rows ? left : rows)};
+        const PlanTile t = p.plan_tiles[tile];
+        return {t.expert, t.first, t.count};
     }
-    return true;
+    const int64_t first = (int64_t)tile * rows, left = p.n_rows - first;
+    return {0, first, (int32_t)(left < rows ? left : rows)};
 }
-__device__ __forceinline__ int64_t x_row(const MmParams &p, int64_t at) { return p.order ? p.order[at] / p.divide : at; }
+__device__ __forceinline__ int64_t x_row(const MmParams &p, int64_t y_row) { return p.order ? (int64_t)((uint64_t)y_row * p.divide >> p.divide_shift) : y_row; }
 __device__ __forceinline__ int64_t y_row(const MmParams &p, int64_t at) { return p.order ? p.order[at] : at; }
 
 // ---- few rows: 16 of them times two rows of tiles, by four waves that share the columns.  The sums of the waves are added in their order.
@@ -186,12 +195,13 @@ __global__ void __launch_bounds__(64 * kFewWaves) q4_few_kernel(const MmParams p
 {
     __shared__ float sums[kFewWaves][2][16][17];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, q = lane >> 4;
-    RowTile rt;
-    if (!row_tile(p, blockIdx.x / p.col_blocks, 16, rt)) return;
+    const RowTile rt = row_tile(p, blockIdx.x / p.col_blocks, 16);
+    if (rt.count == 0) return;
+    const SixteenPlus<DT> sixteen_plus;
     const int col_block = blockIdx.x % p.col_blocks;
     const int64_t last = p.tile_rows - 1, r0 = 2 * (int64_t)col_block, r1 = r0 < last ? r0 + 1 : r0;
     const int64_t row[2] = {rt.mat * p.tile_rows + r0, rt.mat * p.tile_rows + r1};
-    const uint16_t *x = p.X + (n < rt.count ? x_row(p, rt.first + n) : 0) * p.ldx + 8 * q;
+    const uint16_t *x = p.X + (n < rt.count ? x_row(p, y_row(p, rt.first + n)) : 0) * p.ldx + 8 * q;
 
     float4v acc[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
     const float4v none = {0, 0, 0, 0};
@@ -219,7 +229,7 @@ __global__ void __launch_bounds__(64 * kFewWaves) q4_few_kernel(const MmParams p
             for (int i = c; i < c + CH; ++i) {
                 of_x = mfma16x16x32<DT>(xf[i], ones, of_x);
 #pragma unroll
-                for (int h = 0; h < 2; ++h) part[h] = mfma16x16x32<DT>(xf[i], sixteen_plus<DT>(w[h][i]), part[h]);
+                for (int h = 0; h < 2; ++h) part[h] = mfma16x16x32<DT>(xf[i], sixteen_plus(w[h][i]), part[h]);
             }
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -286,9 +296,11 @@ __global__ void __launch_bounds__(256, 2) q4_many_kernel(const MmParams p)
     constexpr int kRows = 16 * MT, kGroups = 4 / CH, NT = kManyRows;
     __shared__ __attribute__((aligned(16))) uint4v x_lds[2][kRows * 16];         // chunk c of row r at r * 16 + (c ^ r % 16)
     __shared__ float sum_lds[2][4][kRows];                                       // of four groups in turn
+    __shared__ int64_t y_lds[kRows];                                             // where the rows of Y begin
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, q = lane >> 4;
-    RowTile rt;
-    if (!row_tile(p, blockIdx.x / p.col_blocks, kRows, rt)) return;
+    const RowTile rt = row_tile(p, blockIdx.x / p.col_blocks, kRows);
+    if (rt.count == 0) return;
+    const SixteenPlus<DT> sixteen_plus;
     const int64_t last = p.tile_rows - 1, r0 = ((int64_t)(blockIdx.x % p.col_blocks) * 4 + wave) * NT;
     // W from the wave's first row of tiles on (behind the last one, that one), 32-bit offsets from there
     const int64_t from = rt.mat * p.tile_rows + (r0 < last ? r0 : last);
@@ -302,13 +314,27 @@ __global__ void __launch_bounds__(256, 2) q4_many_kernel(const MmParams p)
         s_row[h] = (uint32_t)((h < further ? h : further) * p.steps) * 16u;
     }
 
+    uint4v w[NT];
+    Words<kGroups> sz[NT];
+    auto fetch_w = [&](int h, int t) {
+        w[h] = *reinterpret_cast<const uint4v *>(w_at + (w_row[h] + (uint32_t)t * 1024u + (uint32_t)lane * 16u));
+        const uint32_t at = s_row[h] + (uint32_t)(t / p.tiles_a_step) * 16u + (uint32_t)n;
+        sz[h].s = *reinterpret_cast<const typename Words<kGroups>::Scales *>(s_at + at * (2u * kGroups));
+        if constexpr (ZEROS) sz[h].z = *reinterpret_cast<const typename Words<kGroups>::Zeros *>(z_at + at * (uint32_t)kGroups);
+    };
+#pragma unroll
+    for (int h = 0; h < NT; ++h) fetch_w(h, 0);
+
     // this thread's chunks of X: chunk c of rows xr + 16 j
     const int c = threadIdx.x & 15, xr = threadIdx.x >> 4;
     const uint16_t *src[MT];
 #pragma unroll
-    for (int j = 0; j < MT; ++j) src[j] = p.X + x_row(p, rt.first + (xr + 16 * j < rt.count ? xr + 16 * j : 0)) * p.ldx + 8 * c;
-    uint4v xv[MT], w[NT];
-    Words<kGroups> sz[NT];
+    for (int j = 0; j < MT; ++j) {
+        const int64_t row = y_row(p, rt.first + (xr + 16 * j < rt.count ? xr + 16 * j : 0));
+        if (c == 0) y_lds[xr + 16 * j] = row * p.ldy;
+        src[j] = p.X + x_row(p, row) * p.ldx + 8 * c;
+    }
+    uint4v xv[MT];
     auto fetch_x = [&](int t) {
 #pragma unroll
         for (int j = 0; j < MT; ++j) {
@@ -328,12 +354,6 @@ __global__ void __launch_bounds__(256, 2) q4_many_kernel(const MmParams p)
             if (c % (4 * CH) == 0) sum_lds[g >> 2 & 1][g & 3][xr + 16 * j] = s;
         }
     };
-    auto fetch_w = [&](int h, int t) {
-        w[h] = *reinterpret_cast<const uint4v *>(w_at + (w_row[h] + (uint32_t)t * 1024u + (uint32_t)lane * 16u));
-        const uint32_t at = s_row[h] + (uint32_t)(t / p.tiles_a_step) * 16u + (uint32_t)n;
-        sz[h].s = *reinterpret_cast<const typename Words<kGroups>::Scales *>(s_at + at * (2u * kGroups));
-        if constexpr (ZEROS) sz[h].z = *reinterpret_cast<const typename Words<kGroups>::Zeros *>(z_at + at * (uint32_t)kGroups);
-    };
     float4v acc[MT][NT];
 #pragma unroll
     for (int m = 0; m < MT; ++m)
@@ -344,8 +364,6 @@ __global__ void __launch_bounds__(256, 2) q4_many_kernel(const MmParams p)
     for (int h = 0; h < NT; ++h) taken[h] = 0.f;
     const int n_tiles = (int)p.k_tiles;
     fetch_x(0);
-#pragma unroll
-    for (int h = 0; h < NT; ++h) fetch_w(h, 0);
     put_x(0);
     __syncthreads();
     for (int t = 0; t < n_tiles; ++t) {
@@ -366,12 +384,16 @@ __global__ void __launch_bounds__(256, 2) q4_many_kernel(const MmParams p)
                 for (int m = 0; m < MT; ++m) part[m] = float4v{0, 0, 0, 0};
 #pragma unroll
                 for (int i = 0; i < CH; ++i) {
-                    const short8v b = sixteen_plus<DT>(w[h][g * CH + i]);
+                    const short8v b = sixteen_plus(w[h][g * CH + i]);
 #pragma unroll
                     for (int m = 0; m < MT; ++m) part[m] = mfma16x16x32<DT>(xf[m][i], b, part[m]);
                 }
                 const float s = sz[h].template scale<DT>(g);
-                taken[h] = q == slot ? s * (ZEROS ? sz[h].minus_sixteen_plus_zero(g) : -24.f) : taken[h];
+                if constexpr (CH == 1) {
+                    if (g == 0) taken[h] = sz[h].template scale<DT>(q) * (ZEROS ? sz[h].minus_sixteen_plus_zero(q) : -24.f);
+                } else {
+                    taken[h] = q == slot ? s * (ZEROS ? sz[h].minus_sixteen_plus_zero(g) : -24.f) : taken[h];
+                }
                 if (g == kGroups - 1) fetch_w(h, next);           // a step ahead, into the registers just read
 #pragma unroll
                 for (int m = 0; m < MT; ++m)
@@ -400,7 +422,7 @@ __global__ void __launch_bounds__(256, 2) q4_many_kernel(const MmParams p)
         for (int i = 0; i < 4; ++i) {
             const int token = 16 * m + 4 * q + i;
             if (token >= rt.count) continue;
-            const int64_t at = y_row(p, rt.first + token) * p.ldy;
+            const int64_t at = y_lds[token];
             if (p.gated) {
 #pragma unroll
                 for (int h = 0; h < NT; h += 2) {
@@ -574,10 +596,13 @@ extern "C" int q4_mm_routed(const q4_t *h, const void *plan_dev, int64_t n_pairs
     MmParams p = mm_params(h, X_dev, ldx, Y_dev, ldy, n_pairs);
     const PlanParts parts = plan_parts(n_pairs, (int32_t)h->n_mats);
     const char *d = static_cast<const char *>(plan_dev);
-    p.offsets = reinterpret_cast<const int32_t *>(d);
     p.order = reinterpret_cast<const int32_t *>(d + parts.order);
-    p.plan_tiles = reinterpret_cast<const int2 *>(d + parts.tiles);
-    p.divide = (int32_t)(n_pairs / n_rows);
+    p.plan_tiles = reinterpret_cast<const PlanTile *>(d + parts.tiles);
+    // i / d for i below 2^31: 2^(31 + l) / d rounded up, l the bits of d - 1
+    const int64_t d_rows = n_pairs / n_rows;
+    const int l = d_rows > 1 ? 64 - __builtin_clzll((unsigned long long)d_rows - 1) : 0;
+    p.divide = (uint32_t)(((1ull << (31 + l)) + d_rows - 1) / d_rows);
+    p.divide_shift = 31 + l;
     p.f32 = y_type == VBR_F32;
     return launch_mm(h, p, parts.tile_rows, parts.n_tiles, hip_stream);
 }

@@ -12,8 +12,11 @@ constexpr int32_t kMaxTopK = 64, kMaxGroups = 64;  // one lane each
 constexpr int64_t kMaxPairs = 1 << 30;             // positions are 32 bits
 constexpr int32_t kPlanChunk = 1024;               // pairs a wave counts
 
-// Byte offsets in a plan: int32 offsets [n_experts + 1] at 0, int32 order [n_pairs], int2 tiles [n_tiles] (expert or -1, first position),
+// Byte offsets in a plan: int32 offsets [n_experts + 1] at 0, int32 order [n_pairs], PlanTile tiles [n_tiles],
 // int32 counts [n_chunks][n_experts].
+struct PlanTile {
+    int32_t expert, first, count, unused;          // positions first .. first + count - 1 of the order; count 0: no tile
+};
 struct PlanParts {
     int64_t order, tiles, counts, total;
     int64_t n_tiles, n_chunks;

@@ -298,7 +298,7 @@ __device__ __forceinline__ int expert_of(const int32_t *ids, int64_t at, int64_t
 struct PlanParams {
     const int32_t *ids;
     int32_t *offsets, *order, *counts;             // counts [n_chunks][n_experts]
-    int2 *tiles;
+    PlanTile *tiles;
     int64_t n_pairs;
     int32_t n_experts, bits, n_chunks, tile_rows, n_tiles;
 };
@@ -363,8 +363,11 @@ __global__ void __launch_bounds__(kScanThreads) plan_scan_kernel(const PlanParam
     }
     if (e == 0) p.offsets[p.n_experts] = total;
     const int tiles = (count + p.tile_rows - 1) / p.tile_rows, tile = scan_1024(tiles, sums, n_tiles);
-    for (int i = 0; i < tiles; ++i) p.tiles[tile + i] = make_int2(e, start + i * p.tile_rows);
-    for (int i = n_tiles + e; i < p.n_tiles; i += kScanThreads) p.tiles[i] = make_int2(-1, 0);
+    for (int i = 0; i < tiles; ++i) {
+        const int left = count - i * p.tile_rows;
+        p.tiles[tile + i] = {e, start + i * p.tile_rows, left < p.tile_rows ? left : p.tile_rows, 0};
+    }
+    for (int i = n_tiles + e; i < p.n_tiles; i += kScanThreads) p.tiles[i] = {0, 0, 0, 0};
     for (int64_t i = total + (int64_t)e; i < p.n_pairs; i += kScanThreads) p.order[i] = -1;
 }
 
@@ -551,7 +554,7 @@ PlanParts plan_parts(int64_t n_pairs, int32_t n_experts)
     q.n_chunks = (n_pairs + kPlanChunk - 1) / kPlanChunk;
     q.order = up(4 * ((int64_t)n_experts + 1), 256);
     q.tiles = up(q.order + 4 * n_pairs, 256);
-    q.counts = up(q.tiles + 8 * q.n_tiles, 256);
+    q.counts = up(q.tiles + (int64_t)sizeof(PlanTile) * q.n_tiles, 256);
     q.total = up(q.counts + 4 * q.n_chunks * n_experts, 256);
     return q;
 }
@@ -639,7 +642,7 @@ extern "C" int route_plan(const int32_t *ids_dev, int64_t n_pairs, int32_t n_exp
     p.ids = ids_dev;
     p.offsets = reinterpret_cast<int32_t *>(d);
     p.order = reinterpret_cast<int32_t *>(d + q.order);
-    p.tiles = reinterpret_cast<int2 *>(d + q.tiles);
+    p.tiles = reinterpret_cast<PlanTile *>(d + q.tiles);
     p.counts = reinterpret_cast<int32_t *>(d + q.counts);
     p.n_pairs = n_pairs;
     p.n_experts = n_experts;
