@@ -8,6 +8,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <cstdlib>
 #include <new>
 #include <type_traits>
 
@@ -96,7 +97,7 @@ struct MmParams {
     int64_t ldx, ldy, n_rows;                  // rows of Y
     int64_t k_tiles, tile_rows, steps;
     int32_t half, k_chunks, tiles_a_step;      // k_chunks: columns / 32
-    int32_t gated, f32;
+    int32_t gated, f32, fours;                 // fours: four elements of Y from a multiple of four on are aligned to as much
     int32_t col_blocks, row_tiles;             // of the launch; row_tiles: at most so many, if routed
     // routed, or null
     const PlanTile *plan_tiles;
@@ -169,6 +170,27 @@ __device__ __forceinline__ void store_y(const MmParams &p, int64_t at, float y)
     else static_cast<__bf16 *>(p.Y)[at] = (__bf16)y;
 }
 
+// four columns of a row that begins at element `row`; they are stored together where that is a whole number of them
+template <int DT>
+__device__ __forceinline__ void store_4(const MmParams &p, int64_t row, int64_t col, float4v y)
+{
+    if (p.fours && col + 4 <= p.half) {
+        if (p.f32) {
+            *reinterpret_cast<float4v *>(static_cast<float *>(p.Y) + row + col) = y;
+        } else if constexpr (DT == VBR_F16) {
+            typedef _Float16 half4v __attribute__((ext_vector_type(4)));
+            *reinterpret_cast<half4v *>(static_cast<_Float16 *>(p.Y) + row + col) = __builtin_convertvector(y, half4v);
+        } else {
+            typedef __bf16 bf16x4v __attribute__((ext_vector_type(4)));
+            *reinterpret_cast<bf16x4v *>(static_cast<__bf16 *>(p.Y) + row + col) = __builtin_convertvector(y, bf16x4v);
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (col + i < p.half) store_y<DT>(p, row + col + i, y[i]);
+}
+
 // rows first .. first + count - 1 (positions of the plan's order, if routed) of matrix mat
 struct RowTile {
     int64_t mat, first;
@@ -185,92 +207,6 @@ __device__ __forceinline__ RowTile row_tile(const MmParams &p, int tile, int row
 }
 __device__ __forceinline__ int64_t x_row(const MmParams &p, int64_t y_row) { return p.order ? (int64_t)((uint64_t)y_row * p.divide >> p.divide_shift) : y_row; }
 __device__ __forceinline__ int64_t y_row(const MmParams &p, int64_t at) { return p.order ? p.order[at] : at; }
-
-// ---- few rows: 16 of them times two rows of tiles, by four waves that share the columns.  The sums of the waves are added in their order.
-// CH: steps of 32 columns between applications of a scale (1, 2, or 4)
-constexpr int kFewWaves = 4;
-
-template <int DT, int CH, bool ZEROS>
-__global__ void __launch_bounds__(64 * kFewWaves) q4_few_kernel(const MmParams p)
-{
-    __shared__ float sums[kFewWaves][2][16][17];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, q = lane >> 4;
-    const RowTile rt = row_tile(p, blockIdx.x / p.col_blocks, 16);
-    if (rt.count == 0) return;
-    const SixteenPlus<DT> sixteen_plus;
-    const int col_block = blockIdx.x % p.col_blocks;
-    const int64_t last = p.tile_rows - 1, r0 = 2 * (int64_t)col_block, r1 = r0 < last ? r0 + 1 : r0;
-    const int64_t row[2] = {rt.mat * p.tile_rows + r0, rt.mat * p.tile_rows + r1};
-    const uint16_t *x = p.X + (n < rt.count ? x_row(p, y_row(p, rt.first + n)) : 0) * p.ldx + 8 * q;
-
-    float4v acc[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
-    const float4v none = {0, 0, 0, 0};
-    const short one = DT == VBR_F16 ? 0x3C00 : 0x3F80;
-    const short8v ones = {one, one, one, one, one, one, one, one};
-    const int begin = (int)(p.k_tiles * wave / kFewWaves), end = (int)(p.k_tiles * (wave + 1) / kFewWaves);
-    for (int t = begin; t < end; ++t) {
-        uint4v w[2];
-        Words<4 / CH> sz[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            w[h] = p.tiles[(row[h] * p.k_tiles + t) * 64 + lane];
-            sz[h] = load_words<4 / CH, ZEROS>(p, row[h], t / p.tiles_a_step, n);
-        }
-        short8v xf[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            xf[i] = short8v{0, 0, 0, 0, 0, 0, 0, 0};
-            if (n < rt.count && 4 * t + i < p.k_chunks) xf[i] = *reinterpret_cast<const short8v *>(x + 128 * (int64_t)t + 32 * i);
-        }
-#pragma unroll
-        for (int c = 0; c < 4; c += CH) {
-            float4v of_x = none, part[2] = {none, none};
-#pragma unroll
-            for (int i = c; i < c + CH; ++i) {
-                of_x = mfma16x16x32<DT>(xf[i], ones, of_x);
-#pragma unroll
-                for (int h = 0; h < 2; ++h) part[h] = mfma16x16x32<DT>(xf[i], sixteen_plus(w[h][i]), part[h]);
-            }
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const float s = sz[h].template scale<DT>(c / CH), z = ZEROS ? sz[h].minus_sixteen_plus_zero(c / CH) : -24.f;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) acc[h][i] = __builtin_fmaf(s, __builtin_fmaf(z, of_x[i], part[h][i]), acc[h][i]);
-            }
-        }
-    }
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) sums[wave][h][4 * q + i][n] = acc[h][i];
-    __syncthreads();
-    const int outs = p.gated ? 1 : 2;
-    for (int at = threadIdx.x; at < outs * 256; at += 64 * kFewWaves) {
-        const int col = at & 15, token = at >> 4 & 15, h = at >> 8;
-        const int64_t out_col = (p.gated ? col_block : r0 + h) * 16 + col;
-        if (token >= rt.count || out_col >= p.half || (!p.gated && r0 + h > last)) continue;
-        float v = 0.f;
-#pragma unroll
-        for (int k = 0; k < kFewWaves; ++k) v += sums[k][h][token][col];
-        if (p.gated) {
-            float u = 0.f;
-#pragma unroll
-            for (int k = 0; k < kFewWaves; ++k) u += sums[k][1][token][col];
-            v = silu(v) * u;
-        }
-        store_y<DT>(p, y_row(p, rt.first + token) * p.ldy + out_col, v);
-    }
-}
-
-// ---- many rows: 16 MT of them times 16 rows of tiles, by four waves with four rows of tiles each.  A step is a tile's 128 columns: X goes through LDS,
-// which all waves read; W comes straight into registers, as it was laid out, and is turned into numbers there.
-constexpr int kManyRows = 4;           // rows of tiles a wave
-
-template <int CTRL>
-__device__ __forceinline__ float add_lane(float x)
-{
-    return x + __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
-}
 
 typedef _Float16 half2v __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2v __attribute__((ext_vector_type(2)));
@@ -290,6 +226,355 @@ __device__ __forceinline__ float sum_of_8(uint4v x)
 
 // What (16 + z) takes from a sum is a product itself, of the sums of x in a group and s (16 + z): four groups at a time it goes to the matrix units in
 // fp32, so that the vector units have one multiplication and addition a sum and group.
+
+__device__ __forceinline__ float sum_over_quarters(float x)           // of lanes n, 16 + n, 32 + n and 48 + n, in all four
+{
+    const auto a = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+    const float y = __builtin_bit_cast(float, (uint32_t)a[0]) + __builtin_bit_cast(float, (uint32_t)a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, y), __builtin_bit_cast(uint32_t, y), false, false);
+    return __builtin_bit_cast(float, (uint32_t)b[0]) + __builtin_bit_cast(float, (uint32_t)b[1]);
+}
+
+// ---- few workgroups' worth of rows: 16 MT rows of X times NT rows of tiles, by waves that share the columns, each with a range of steps of its own.  Nothing is
+// shared before the end, where the sums of the waves are added in their order: X comes from the L2 into registers, AHEAD_X steps ahead, W AHEAD_W.
+// CH: steps of 32 columns between applications of a scale (1, 2, or 4)
+// sums [n_waves][NT][row][kSumRow], so that a lane's four are 16 bytes and rows fall on different banks; added in the waves' order and stored
+constexpr int kSumRow = 20;
+template <int DT, int NT, int ROWS>
+__device__ __forceinline__ void store_sums(const MmParams &p, const RowTile &rt, int64_t r0, const float *sums, int n_waves)
+{
+    const int halves = p.gated ? 2 : 1, lg = (NT == 1 ? 2 : NT == 2 ? 3 : 4) - (p.gated ? 1 : 0);      // 2^lg threads have four columns each of a row
+    const int h0 = (threadIdx.x >> 2 & ((1 << (lg - 2)) - 1)) * halves, c0 = (threadIdx.x & 3) * 4;
+    const int64_t out_col = ((r0 + h0) >> (halves - 1)) * 16 + c0;
+    for (int token = threadIdx.x >> lg; token < rt.count; token += blockDim.x >> lg) {
+        auto sum = [&](int h) {
+            float4v v = {0, 0, 0, 0};
+            for (int k = 0; k < n_waves; ++k) v += *reinterpret_cast<const float4v *>(sums + ((k * NT + h) * ROWS + token) * kSumRow + c0);
+            return v;
+        };
+        float4v v = sum(h0);
+        if (p.gated) {
+            const float4v up = sum(h0 + 1);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = silu(v[i]) * up[i];
+        }
+        store_4<DT>(p, y_row(p, rt.first + token) * p.ldy, out_col, v);
+    }
+}
+
+template <int DT, int CH, bool ZEROS, int MT, int NT, int AHEAD_W, int AHEAD_X, int THREADS>
+__global__ void __launch_bounds__(THREADS) q4_split_kernel(const MmParams p)
+{
+    constexpr int kGroups = 4 / CH, kRows = 16 * MT;
+    extern __shared__ __attribute__((aligned(16))) float sums[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n_waves = blockDim.x >> 6, n = lane & 15, q = lane >> 4;
+    const RowTile rt = row_tile(p, blockIdx.x / p.col_blocks, kRows);
+    if (rt.count == 0) return;
+    const SixteenPlus<DT> sixteen_plus;
+    const int64_t last = p.tile_rows - 1, r0 = (int64_t)(blockIdx.x % p.col_blocks) * NT;
+    const int further = (int)(last - r0 < NT ? last - r0 : NT - 1);
+    const int64_t from = rt.mat * p.tile_rows + r0;
+    const char *w_at = reinterpret_cast<const char *>(p.tiles) + from * p.k_tiles * 1024;
+    const char *s_at = p.scales + from * p.steps * (32 * kGroups), *z_at = p.zeros + from * p.steps * (16 * kGroups);
+    // The steps of a wave, begun at another one in every workgroup: rows of X and W are powers of two apart more often than not, and what is read at the
+    // same time should not lie in the same channels.
+    const int n_tiles = (int)p.k_tiles, begin = (int)((int64_t)n_tiles * wave / n_waves), n_steps = (int)((int64_t)n_tiles * (wave + 1) / n_waves) - begin;
+    const int turn = n_steps > 0 ? (int)(blockIdx.x % p.col_blocks) % n_steps : 0;
+    auto tile_of = [&](int u) {                                        // (a wave without steps fetches, too: a tile that is there)
+        const int v = (u < n_steps ? u : n_steps > 0 ? n_steps - 1 : 0) + turn, t = begin + (v < n_steps ? v : v - n_steps);
+        return t < n_tiles ? t : n_tiles - 1;
+    };
+
+    uint4v w[AHEAD_W][NT];
+    Words<kGroups> sz[AHEAD_W][NT];
+    short8v xf[AHEAD_X][MT][4];
+    auto fetch_w = [&](auto d, int h, int t) {
+        const uint32_t hh = h < further ? h : further;
+        w[d][h] = *reinterpret_cast<const uint4v *>(w_at + ((hh * (uint32_t)n_tiles + (uint32_t)t) * 1024u + (uint32_t)lane * 16u));
+        const uint32_t at = (hh * (uint32_t)p.steps + (uint32_t)(t / p.tiles_a_step)) * 16u + (uint32_t)n;
+        sz[d][h].s = *reinterpret_cast<const typename Words<kGroups>::Scales *>(s_at + at * (2u * kGroups));
+        if constexpr (ZEROS) sz[d][h].z = *reinterpret_cast<const typename Words<kGroups>::Zeros *>(z_at + at * (uint32_t)kGroups);
+    };
+    static_for<AHEAD_W>([&](auto d) {
+#pragma unroll
+        for (int h = 0; h < NT; ++h) fetch_w(d, h, tile_of(d));
+    });
+    // rows behind the last one are that of the first again, and never stored
+    const uint16_t *x[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) x[m] = p.X + x_row(p, y_row(p, rt.first + (16 * m + n < rt.count ? 16 * m + n : 0))) * p.ldx + 8 * q;
+    auto fetch_x = [&](auto d, int t) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int chunk = 4 * t + i < p.k_chunks ? 4 * t + i : p.k_chunks - 1;
+#pragma unroll
+            for (int m = 0; m < MT; ++m) xf[d][m][i] = *reinterpret_cast<const short8v *>(x[m] + 32 * (int64_t)chunk);
+        }
+    };
+    static_for<AHEAD_X>([&](auto d) { fetch_x(d, tile_of(d)); });
+
+    float4v acc[MT][NT];
+    float taken[NT], of_x[MT];                                         // -s (16 + z) and the sum of x of the q-th of four groups
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int h = 0; h < NT; ++h) acc[m][h] = float4v{0, 0, 0, 0};
+#pragma unroll
+    for (int h = 0; h < NT; ++h) taken[h] = 0.f;
+#pragma unroll
+    for (int m = 0; m < MT; ++m) of_x[m] = 0.f;
+    auto take = [&]() {
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int h = 0; h < NT; ++h) acc[m][h] = __builtin_amdgcn_mfma_f32_16x16x4f32(of_x[m], taken[h], acc[m][h], 0, 0, 0);
+#pragma unroll
+        for (int h = 0; h < NT; ++h) taken[h] = 0.f;
+    };
+    auto step = [&](auto d, auto more_w, auto more_x, int u) {
+        constexpr int dx = d.value % AHEAD_X;
+        const int t = tile_of(u);
+        if (4 * t + 4 > p.k_chunks) {                              // the last columns are fewer
+#pragma unroll
+            for (int i = 1; i < 4; ++i)
+                if (4 * t + i >= p.k_chunks) {
+#pragma unroll
+                    for (int m = 0; m < MT; ++m) xf[dx][m][i] = short8v{0, 0, 0, 0, 0, 0, 0, 0};
+                }
+        }
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) {
+            const int slot = ((AHEAD_W % 4 == 0 ? d.value : u) * kGroups + g) & 3;
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                float s = 0.f;
+#pragma unroll
+                for (int i = g * CH; i < (g + 1) * CH; ++i) s += sum_of_8<DT>(__builtin_bit_cast(uint4v, xf[dx][m][i]));
+                s = sum_over_quarters(s);
+                of_x[m] = q == slot ? s : of_x[m];
+            }
+#pragma unroll
+            for (int h = 0; h < NT; ++h) {
+                float4v part[MT];
+#pragma unroll
+                for (int m = 0; m < MT; ++m) part[m] = float4v{0, 0, 0, 0};
+#pragma unroll
+                for (int i = g * CH; i < (g + 1) * CH; ++i) {
+                    const short8v b = sixteen_plus(w[d][h][i]);
+#pragma unroll
+                    for (int m = 0; m < MT; ++m) part[m] = mfma16x16x32<DT>(xf[dx][m][i], b, part[m]);
+                }
+                const float s = sz[d][h].template scale<DT>(g);
+                if constexpr (CH == 1) {
+                    if (g == 0) taken[h] = sz[d][h].template scale<DT>(q) * (ZEROS ? sz[d][h].minus_sixteen_plus_zero(q) : -24.f);
+                } else {
+                    taken[h] = q == slot ? s * (ZEROS ? sz[d][h].minus_sixteen_plus_zero(g) : -24.f) : taken[h];
+                }
+                if (more_w.value && g == kGroups - 1) fetch_w(d, h, tile_of(u + AHEAD_W));
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[m][h][i] = __builtin_fmaf(s, part[m][i], acc[m][h][i]);
+            }
+            if (g == kGroups - 1 && slot == 3) take();
+            if constexpr (MT > 1) __builtin_amdgcn_sched_barrier(0);
+        }
+        if constexpr (more_x.value) fetch_x(constant<dx>(), tile_of(u + AHEAD_X));
+    };
+    // No load stands in a branch, so that every wait is for the oldest ones and not for all.
+    int first = 0;
+    for (; first + AHEAD_W < n_steps; first += AHEAD_W)
+        static_for<AHEAD_W>([&](auto d) { step(d, constant<1>(), constant<1>(), first + d); });
+    static_for<AHEAD_W>([&](auto d) {
+        if (first + d < n_steps) step(d, constant<0>(), constant<(d.value + AHEAD_X < AHEAD_W)>(), first + d);
+    });
+    if constexpr (CH > 1) take();                                      // what is left of four groups; of the others taken is zero
+    float *mine = sums + (int64_t)wave * NT * kRows * kSumRow;
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int h = 0; h < NT; ++h)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) mine[(h * kRows + 16 * m + 4 * q + i) * kSumRow + n] = acc[m][h][i];
+    __syncthreads();
+    store_sums<DT, NT, kRows>(p, rt, r0, sums, n_waves);
+}
+
+// ---- more rows than 16, and few workgroups: the same division of the work, with X through a part of LDS that each wave has for itself.  A wave's load
+// takes 256 bytes of four rows (the pieces of 64 bytes that the matrix units take are half a line each, and the other half is gone from the L1 before it is
+// asked for).  The rows of a step are read into registers at once and those of the next step fetched into their place.
+template <int DT, int CH, bool ZEROS, int MT>
+__global__ void __launch_bounds__(512) q4_mid_kernel(const MmParams p)
+{
+    constexpr int kGroups = 4 / CH, kRows = 16 * MT, NT = 4;
+    extern __shared__ __attribute__((aligned(16))) float sums[];
+    __shared__ const char *row_lds[kRows];                             // where the rows of X begin
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n_waves = blockDim.x >> 6, n = lane & 15, q = lane >> 4;
+    const RowTile rt = row_tile(p, blockIdx.x / p.col_blocks, kRows);
+    if (rt.count == 0) return;
+    const SixteenPlus<DT> sixteen_plus;
+    const int64_t last = p.tile_rows - 1, r0 = (int64_t)(blockIdx.x % p.col_blocks) * NT;
+    const int further = (int)(last - r0 < NT ? last - r0 : NT - 1);
+    const int64_t from = rt.mat * p.tile_rows + r0;
+    const char *w_at = reinterpret_cast<const char *>(p.tiles) + from * p.k_tiles * 1024;
+    const char *s_at = p.scales + from * p.steps * (32 * kGroups), *z_at = p.zeros + from * p.steps * (16 * kGroups);
+    const int n_tiles = (int)p.k_tiles, begin = (int)((int64_t)n_tiles * wave / n_waves), n_steps = (int)((int64_t)n_tiles * (wave + 1) / n_waves) - begin;
+    const int turn = n_steps > 0 ? (int)(blockIdx.x % p.col_blocks) % n_steps : 0;
+    auto tile_of = [&](int u) {
+        const int v = (u < n_steps ? u : n_steps > 0 ? n_steps - 1 : 0) + turn, t = begin + (v < n_steps ? v : v - n_steps);
+        return t < n_tiles ? t : n_tiles - 1;
+    };
+    uint4v w[NT];
+    Words<kGroups> sz[NT];
+    auto fetch_w = [&](int h, int t) {
+        const uint32_t hh = h < further ? h : further;
+        w[h] = *reinterpret_cast<const uint4v *>(w_at + ((hh * (uint32_t)n_tiles + (uint32_t)t) * 1024u + (uint32_t)lane * 16u));
+        const uint32_t at = (hh * (uint32_t)p.steps + (uint32_t)(t / p.tiles_a_step)) * 16u + (uint32_t)n;
+        sz[h].s = *reinterpret_cast<const typename Words<kGroups>::Scales *>(s_at + at * (2u * kGroups));
+        if constexpr (ZEROS) sz[h].z = *reinterpret_cast<const typename Words<kGroups>::Zeros *>(z_at + at * (uint32_t)kGroups);
+    };
+    // rows behind the last one are the first again, and never stored
+    if (threadIdx.x < kRows)
+        row_lds[threadIdx.x] = reinterpret_cast<const char *>(p.X + x_row(p, y_row(p, rt.first + ((int)threadIdx.x < rt.count ? threadIdx.x : 0))) * p.ldx);
+    __syncthreads();
+    // chunk c of row r of this wave's part is at 16 (16 r + (c ^ r % 16)); lane l of load j takes what comes to row 4 j + l / 16, place l % 16
+    uint4v *mine_x = reinterpret_cast<uint4v *>(sums) + wave * (kRows * 16);
+    const uint32_t x_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint4v *)mine_x;
+    auto fetch_x = [&](int t) {
+        const uint32_t left = (uint32_t)(p.k_chunks - 4 * t) * 4u - 1u;       // the last chunk that is there
+        static_for<4 * MT>([&](auto j) {
+            uint32_t c = (uint32_t)n ^ (uint32_t)(4 * (j.value & 3) + q);
+            c = c < left ? c : left;
+            const char *src = row_lds[4 * j.value + q] + ((uint32_t)t * 256u + c * 16u);
+            dma16(src, x_base + j.value * 1024);
+        });
+    };
+    fetch_x(tile_of(0));
+#pragma unroll
+    for (int h = 0; h < NT; ++h) fetch_w(h, tile_of(0));
+    float4v acc[MT][NT];
+    float taken[NT], of_x[MT];                                         // -s (16 + z) and the sum of x of the q-th of four groups
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int h = 0; h < NT; ++h) acc[m][h] = float4v{0, 0, 0, 0};
+#pragma unroll
+    for (int h = 0; h < NT; ++h) taken[h] = 0.f;
+#pragma unroll
+    for (int m = 0; m < MT; ++m) of_x[m] = 0.f;
+    auto take = [&]() {
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int h = 0; h < NT; ++h) acc[m][h] = __builtin_amdgcn_mfma_f32_16x16x4f32(of_x[m], taken[h], acc[m][h], 0, 0, 0);
+#pragma unroll
+        for (int h = 0; h < NT; ++h) taken[h] = 0.f;
+    };
+    for (int u = 0; u < n_steps; ++u) {
+        const int t = tile_of(u), next = tile_of(u + 1);
+        // X of this step is there when nothing but the NT loads of codes behind it is on its way (with them go those of scales and zero points)
+        wait_vmcnt<NT>();
+        short8v xf[MT][4];
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) xf[m][i] = __builtin_bit_cast(short8v, mine_x[(16 * m + n) * 16 + ((4 * i + q) ^ n)]);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");             // read before it is written again
+        fetch_x(next);
+        if (4 * t + 4 > p.k_chunks) {                                  // the last columns are fewer
+#pragma unroll
+            for (int i = 1; i < 4; ++i)
+                if (4 * t + i >= p.k_chunks) {
+#pragma unroll
+                    for (int m = 0; m < MT; ++m) xf[m][i] = short8v{0, 0, 0, 0, 0, 0, 0, 0};
+                }
+        }
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) {
+            const int slot = (u * kGroups + g) & 3;
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                float s = 0.f;
+#pragma unroll
+                for (int i = g * CH; i < (g + 1) * CH; ++i) s += sum_of_8<DT>(__builtin_bit_cast(uint4v, xf[m][i]));
+                s = sum_over_quarters(s);
+                of_x[m] = q == slot ? s : of_x[m];
+            }
+#pragma unroll
+            for (int h = 0; h < NT; ++h) {
+                float4v part[MT];
+#pragma unroll
+                for (int m = 0; m < MT; ++m) part[m] = float4v{0, 0, 0, 0};
+#pragma unroll
+                for (int i = g * CH; i < (g + 1) * CH; ++i) {
+                    const short8v b = sixteen_plus(w[h][i]);
+#pragma unroll
+                    for (int m = 0; m < MT; ++m) part[m] = mfma16x16x32<DT>(xf[m][i], b, part[m]);
+                }
+                const float s = sz[h].template scale<DT>(g);
+                if constexpr (CH == 1) {
+                    if (g == 0) taken[h] = sz[h].template scale<DT>(q) * (ZEROS ? sz[h].minus_sixteen_plus_zero(q) : -24.f);
+                } else {
+                    taken[h] = q == slot ? s * (ZEROS ? sz[h].minus_sixteen_plus_zero(g) : -24.f) : taken[h];
+                }
+                if (g == kGroups - 1) fetch_w(h, next);                // a step ahead, into the registers just read
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[m][h][i] = __builtin_fmaf(s, part[m][i], acc[m][h][i]);
+            }
+            if (g == kGroups - 1 && slot == 3) take();
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+    if constexpr (CH > 1) take();                                      // what is left of four groups; of the others taken is zero
+    // The waves' sums are added pairwise from the back: half of them write, the other half adds, until one is left.
+    wait_vmcnt<0>();                                                   // (the last step fetched its own again)
+    __syncthreads();
+    for (int half = n_waves >> 1; half > 0; half >>= 1) {
+        float *place = sums + (int64_t)(wave - half) * NT * kRows * kSumRow;
+        if (wave >= half && wave < 2 * half) {
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int h = 0; h < NT; ++h)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) place[(h * kRows + 16 * m + 4 * q + i) * kSumRow + n] = acc[m][h][i];
+        }
+        __syncthreads();
+        if (wave < half) {
+            const float *theirs = sums + (int64_t)wave * NT * kRows * kSumRow;
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int h = 0; h < NT; ++h)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[m][h][i] += theirs[(h * kRows + 16 * m + 4 * q + i) * kSumRow + n];
+        }
+        __syncthreads();
+    }
+    if (wave == 0) {
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int h = 0; h < NT; ++h)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sums[(h * kRows + 16 * m + 4 * q + i) * kSumRow + n] = acc[m][h][i];
+    }
+    __syncthreads();
+    store_sums<DT, NT, kRows>(p, rt, r0, sums, 1);
+}
+
+// ---- many rows: 16 MT of them times 16 rows of tiles, by four waves with four rows of tiles each.  A step is a tile's 128 columns: X goes through LDS,
+// which all waves read; W comes straight into registers, as it was laid out, and is turned into numbers there.
+constexpr int kManyRows = 4;           // rows of tiles a wave
+
+template <int CTRL>
+__device__ __forceinline__ float add_lane(float x)
+{
+    return x + __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
+}
+
 template <int DT, int CH, bool ZEROS, int MT>
 __global__ void __launch_bounds__(256, 2) q4_many_kernel(const MmParams p)
 {
@@ -440,17 +725,34 @@ __global__ void __launch_bounds__(256, 2) q4_many_kernel(const MmParams p)
 }
 
 using MmKernel = void (*)(MmParams);
-template <int DT, int CH, bool ZEROS>
-MmKernel mm_kernel(int32_t rows)
+struct Variant {
+    MmKernel kernel;
+    int32_t rows, tile_rows, threads, lds;             // of a workgroup
+};
+template <int DT, int CH, bool ZEROS, int MT, int NT, int AHEAD_W, int AHEAD_X, int THREADS>
+Variant split_variant(int waves)
 {
-    return rows == 16 ? q4_few_kernel<DT, CH, ZEROS> : rows == 32 ? q4_many_kernel<DT, CH, ZEROS, 2> : q4_many_kernel<DT, CH, ZEROS, 4>;
+    return {q4_split_kernel<DT, CH, ZEROS, MT, NT, AHEAD_W, AHEAD_X, THREADS>, 16 * MT, NT, 64 * waves, waves * NT * 16 * MT * kSumRow * 4};
+}
+template <int DT, int CH, bool ZEROS>
+Variant mm_variant(int32_t rows, int split, int waves)
+{
+    if (rows == 16 && split == 1) return split_variant<DT, CH, ZEROS, 1, 1, 4, 2, 1024>(waves);
+    if (rows == 16 && split == 2) return split_variant<DT, CH, ZEROS, 1, 2, 4, 2, 1024>(waves);
+    if (rows == 16) return split_variant<DT, CH, ZEROS, 1, 4, 2, 2, 512>(waves);
+    if (rows == 32 && split == 2) return {q4_mid_kernel<DT, CH, ZEROS, 2>, 32, 4, 64 * waves, waves * 2 * 4096 > waves / 2 * 4 * 32 * kSumRow * 4 ? waves * 2 * 4096 : waves / 2 * 4 * 32 * kSumRow * 4};
+    if (rows == 64 && split == 2) return {q4_mid_kernel<DT, CH, ZEROS, 4>, 64, 4, 64 * waves, waves * 4 * 4096 > waves / 2 * 4 * 64 * kSumRow * 4 ? waves * 4 * 4096 : waves / 2 * 4 * 64 * kSumRow * 4};
+    if (rows == 32 && split) return split_variant<DT, CH, ZEROS, 2, 4, 1, 1, 512>(waves);
+    if (rows == 32) return {q4_many_kernel<DT, CH, ZEROS, 2>, 32, 4 * kManyRows, 256, 0};
+    if (split) return split_variant<DT, CH, ZEROS, 4, 4, 1, 1, 512>(waves);
+    return {q4_many_kernel<DT, CH, ZEROS, 4>, 64, 4 * kManyRows, 256, 0};
 }
 template <int DT>
-MmKernel mm_kernel(int32_t group, bool zeros, int32_t rows)
+Variant mm_variant(int32_t group, bool zeros, int32_t rows, int split, int waves)
 {
-    if (group == 32) return zeros ? mm_kernel<DT, 1, true>(rows) : mm_kernel<DT, 1, false>(rows);
-    if (group == 64) return zeros ? mm_kernel<DT, 2, true>(rows) : mm_kernel<DT, 2, false>(rows);
-    return zeros ? mm_kernel<DT, 4, true>(rows) : mm_kernel<DT, 4, false>(rows);
+    if (group == 32) return zeros ? mm_variant<DT, 1, true>(rows, split, waves) : mm_variant<DT, 1, false>(rows, split, waves);
+    if (group == 64) return zeros ? mm_variant<DT, 2, true>(rows, split, waves) : mm_variant<DT, 2, false>(rows, split, waves);
+    return zeros ? mm_variant<DT, 4, true>(rows, split, waves) : mm_variant<DT, 4, false>(rows, split, waves);
 }
 
 bool aligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
@@ -497,14 +799,22 @@ MmParams mm_params(const q4_t *h, const void *X_dev, int64_t ldx, void *Y_dev, i
     return p;
 }
 
+void set_y(MmParams &p, int32_t y_type)
+{
+    p.f32 = y_type == VBR_F32;
+    p.fours = p.ldy % 4 == 0 && aligned(p.Y, p.f32 ? 16 : 8);
+}
+
 int launch_mm(const q4 *h, MmParams &p, int32_t rows, int64_t row_tiles, void *hip_stream)
 {
-    const int64_t block = rows == 16 ? 2 : 4 * kManyRows;      // rows of tiles of a workgroup
-    p.col_blocks = (int32_t)((p.tile_rows + block - 1) / block);
+    const char *e1 = getenv("Q4_SPLIT"), *e2 = getenv("Q4_WAVES");
+    const int split = e1 ? atoi(e1) : rows == 16 ? 2 : row_tiles * ((p.tile_rows + 15) / 16) < 512 ? 2 : 0;
+    const int waves = e2 ? atoi(e2) : rows == 16 ? 4 : 8;
+    const Variant v = h->dtype == VBR_F16 ? mm_variant<VBR_F16>(h->group, h->zeros, rows, split, waves) : mm_variant<VBR_BF16>(h->group, h->zeros, rows, split, waves);
+    p.col_blocks = (int32_t)((p.tile_rows + v.tile_rows - 1) / v.tile_rows);
     const int64_t grid = row_tiles * p.col_blocks;
     if (grid > INT32_MAX) return VBR_EUNSUPPORTED;
-    const MmKernel kernel = h->dtype == VBR_F16 ? mm_kernel<VBR_F16>(h->group, h->zeros, rows) : mm_kernel<VBR_BF16>(h->group, h->zeros, rows);
-    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(256), 0, static_cast<hipStream_t>(hip_stream), p);
+    hipLaunchKernelGGL(v.kernel, dim3((unsigned)grid), dim3(v.threads), v.lds, static_cast<hipStream_t>(hip_stream), p);
     return launched();
 }
 
@@ -581,7 +891,7 @@ extern "C" int q4_mm(const q4_t *h, const void *X_dev, int64_t ldx, void *Y_dev,
     if (h->n_mats != 1) return VBR_EINVAL;
     if (n_rows == 0) return VBR_OK;
     MmParams p = mm_params(h, X_dev, ldx, Y_dev, ldy, n_rows);
-    p.f32 = y_type == VBR_F32;
+    set_y(p, y_type);
     const int32_t rows = n_rows <= 16 ? 16 : n_rows <= 32 ? 32 : 64;
     return launch_mm(h, p, rows, (n_rows + rows - 1) / rows, hip_stream);
 }
@@ -603,7 +913,7 @@ extern "C" int q4_mm_routed(const q4_t *h, const void *plan_dev, int64_t n_pairs
     const int l = d_rows > 1 ? 64 - __builtin_clzll((unsigned long long)d_rows - 1) : 0;
     p.divide = (uint32_t)(((1ull << (31 + l)) + d_rows - 1) / d_rows);
     p.divide_shift = 31 + l;
-    p.f32 = y_type == VBR_F32;
+    set_y(p, y_type);
     return launch_mm(h, p, parts.tile_rows, parts.n_tiles, hip_stream);
 }
 

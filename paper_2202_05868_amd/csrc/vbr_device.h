@@ -24,6 +24,22 @@ __device__ __forceinline__ float4v mfma16x16x32(short8v a, short8v b, float4v c)
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8v, a), __builtin_bit_cast(bf16x8v, b), c, 0, 0, 0);
 }
 
+// 16 bytes per active lane from global memory straight into LDS, no register staging: lane l's
+// data lands at lds_base + 16 l (lds_base wave-uniform, passed in M0).  The load is counted in
+// vmcnt like any vector load; the compiler does not see it, so the waits are placed by hand.
+// Every wave must issue the same, fixed number of these per K-step (never with an empty lane mask).
+__device__ __forceinline__ void dma16(const void *gptr, uint32_t lds_base)
+{
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(gptr),
+                 "s"((uint32_t)__builtin_amdgcn_readfirstlane(lds_base)) : "memory");
+}
+
+template <int N>
+__device__ __forceinline__ void wait_vmcnt()
+{
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
 template <int I>
 __device__ __forceinline__ uint32_t row_lane(uint32_t x)     // lane I of every row of 16 lanes, to the whole row
 {

@@ -64,16 +64,7 @@ struct Params {
     int32_t split;            // ... and from how many K-steps on these are split
 };
 
-// 16 bytes per active lane from global memory straight into LDS, no register staging: lane l's
-// data lands at lds_base + 16 l (lds_base wave-uniform, passed in M0).  The load is counted in
-// vmcnt like any vector load; the compiler does not see it, so the waits are placed by hand.
-// Every wave must issue the same, fixed number of these per K-step (never with an empty lane mask).
-__device__ __forceinline__ void dma16(const void *gptr, uint32_t lds_base)
-{
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(gptr),
-                 "s"((uint32_t)__builtin_amdgcn_readfirstlane(lds_base)) : "memory");
-}
-// same, address = wave-uniform base + zero-extended 32-bit lane offset
+// dma16 (vbr_device.h) with address = wave-uniform base + zero-extended 32-bit lane offset
 __device__ __forceinline__ void dma16_base(uint32_t voff, const void *base, uint32_t lds_base)
 {
     // the base has to sit in scalar registers: say so explicitly (a no-op when it already does)
@@ -89,12 +80,6 @@ __device__ __forceinline__ void dma4(const void *gptr, uint32_t lds_base)
 {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(gptr),
                  "s"((uint32_t)__builtin_amdgcn_readfirstlane(lds_base)) : "memory");
-}
-
-template <int N>
-__device__ __forceinline__ void wait_vmcnt()
-{
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
 
 // S  = slabs the instantiation computes (tiles of the class have S/2 < n_slabs <= S; 1 for S = 1).
