@@ -7,6 +7,7 @@
 // as a product with ones.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cstdint>
 #include <cstdlib>
 #include <new>
@@ -238,6 +239,12 @@ __device__ __forceinline__ float sum_over_quarters(float x)           // of lane
 // ---- few workgroups' worth of rows: 16 MT rows of X times NT rows of tiles, by waves that share the columns, each with a range of steps of its own.  Nothing is
 // shared before the end, where the sums of the waves are added in their order: X comes from the L2 into registers, AHEAD_X steps ahead, W AHEAD_W.
 // CH: steps of 32 columns between applications of a scale (1, 2, or 4)
+__device__ __forceinline__ float sum_over_halves(float x)             // of lanes n and 32 + n, in both
+{
+    const auto b = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+    return __builtin_bit_cast(float, (uint32_t)b[0]) + __builtin_bit_cast(float, (uint32_t)b[1]);
+}
+
 // sums [n_waves][NT][row][kSumRow], so that a lane's four are 16 bytes and rows fall on different banks; added in the waves' order and stored
 constexpr int kSumRow = 20;
 template <int DT, int NT, int ROWS>
@@ -400,39 +407,141 @@ __global__ void __launch_bounds__(THREADS) q4_split_kernel(const MmParams p)
     store_sums<DT, NT, kRows>(p, rt, r0, sums, n_waves);
 }
 
-// ---- more rows than 16, and few workgroups: the same division of the work, with X through a part of LDS that each wave has for itself.  A wave's load
-// takes 256 bytes of four rows (the pieces of 64 bytes that the matrix units take are half a line each, and the other half is gone from the L1 before it is
-// asked for).  The rows of a step are read into registers at once and those of the next step fetched into their place.
+// ---- more rows than 16: by products of 32 rows with 32 rows of W, which the matrix units take at 1.4 times the rate of those with 16.  Two rows of tiles are
+// side by side: lane 32 h + 16 b + n has row n of the b-th, and of its sixteen blocks of eight columns every second from the h-th on.
+typedef float float16v __attribute__((ext_vector_type(16)));
+
+template <int DT>
+__device__ __forceinline__ float16v mfma32x32x16(short8v a, short8v b, float16v c)
+{
+    if constexpr (DT == VBR_F16)
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8v, a), __builtin_bit_cast(half8v, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8v, a), __builtin_bit_cast(bf16x8v, b), c, 0, 0, 0);
+}
+
+// A wave's part of W: two pairs of rows of tiles from r0 on (behind the last one, that one), and the products with 32 MT rows of X.
+template <int DT, int CH, bool ZEROS, int MT>
+struct Pairs {
+    static constexpr int kGroups = 4 / CH;
+    uint4v w[2][2];
+    Words<kGroups> sz[2];
+    float16v acc[MT][2];
+    float taken[2];                                              // -s (16 + z) of this half's one of two groups
+    SixteenPlus<DT> sixteen_plus;
+    const char *w_at[2], *s_at[2], *z_at[2];
+
+    __device__ __forceinline__ Pairs(const MmParams &p, int64_t mat, int64_t r0, int lane)
+    {
+        const int64_t last = p.tile_rows - 1;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int64_t r = r0 + 2 * h + (lane >> 4 & 1), row = mat * p.tile_rows + (r < last ? r : last);
+            w_at[h] = reinterpret_cast<const char *>(p.tiles) + row * p.k_tiles * 1024 + ((lane & 15) + 16 * (lane >> 5)) * 16;
+            s_at[h] = p.scales + (row * p.steps * 16 + (lane & 15)) * (2 * kGroups);
+            z_at[h] = p.zeros + (row * p.steps * 16 + (lane & 15)) * kGroups;
+#pragma unroll
+            for (int m = 0; m < MT; ++m) acc[m][h] = float16v{};
+            taken[h] = 0.f;
+        }
+    }
+    __device__ __forceinline__ void fetch(const MmParams &p, int h, int t)
+    {
+        w[h][0] = *reinterpret_cast<const uint4v *>(w_at[h] + (uint32_t)t * 1024u);
+        w[h][1] = *reinterpret_cast<const uint4v *>(w_at[h] + (uint32_t)t * 1024u + 512);
+        const uint32_t step = (uint32_t)(t / p.tiles_a_step);
+        sz[h].s = *reinterpret_cast<const typename Words<kGroups>::Scales *>(s_at[h] + step * (32u * kGroups));
+        if constexpr (ZEROS) sz[h].z = *reinterpret_cast<const typename Words<kGroups>::Zeros *>(z_at[h] + step * (16u * kGroups));
+    }
+    // Group g of step u (a tile in the order they are taken), and the fetch of the next one with the last group.  x(m, i): 32 rows and columns 16 i .. of
+    // the tile; of_x(m, g): the sum of x of row m 32 + lane % 32 in this half's one of the groups g - 1 and g.
+    template <class X, class Sums>
+    __device__ __forceinline__ void group(const MmParams &p, int g, int u, int next, bool final, int half, X x, Sums of_x)
+    {
+        const int slot = (CH == 4 ? u : g) & 1;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            float16v part[MT];
+#pragma unroll
+            for (int m = 0; m < MT; ++m) part[m] = float16v{};
+#pragma unroll
+            for (int i = 2 * CH * g; i < 2 * CH * (g + 1); ++i) {
+                const short8v b = sixteen_plus(w[h][i & 1][i >> 1]);
+#pragma unroll
+                for (int m = 0; m < MT; ++m) part[m] = mfma32x32x16<DT>(x(m, i), b, part[m]);
+            }
+            const float s = sz[h].template scale<DT>(g);
+            if constexpr (CH == 4) taken[h] = half == slot ? s * (ZEROS ? sz[h].minus_sixteen_plus_zero(0) : -24.f) : taken[h];
+            else if (slot == 1) taken[h] = sz[h].template scale<DT>(g - 1 + half) * (ZEROS ? sz[h].minus_sixteen_plus_zero(g - 1 + half) : -24.f);
+            if (g == kGroups - 1) fetch(p, h, next);
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[m][h][i] = __builtin_fmaf(s, part[m][i], acc[m][h][i]);
+        }
+        if (slot == 1 || (CH == 4 && final)) {
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                const float sum = half <= slot ? of_x(m, g) : 0.f;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) acc[m][h] = __builtin_amdgcn_mfma_f32_32x32x2f32(sum, half <= slot ? taken[h] : 0.f, acc[m][h], 0, 0, 0);
+            }
+        }
+    }
+};
+
+// 32 rows times 32 columns of sums, the ones of a product's accumulators, to Y: through LDS (32 * kSumRow32 floats that only this wave uses), so that a lane has
+// four columns of a row.  token0: their first row in the tile of rows; y_at(token): where that row of Y begins; r: their first row of tiles.
+constexpr int kSumRow32 = 36;
+template <int DT, class At>
+__device__ __forceinline__ void store_32(const MmParams &p, int count, int token0, int64_t r, float *lds, const float16v &v, int lane, At y_at)
+{
+#pragma unroll
+    for (int i = 0; i < 16; ++i) lds[(8 * (i >> 2) + 4 * (lane >> 5) + (i & 3)) * kSumRow32 + (lane & 31)] = v[i];
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if (p.gated) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int token = 16 * j + (lane >> 2), c = 4 * (lane & 3);
+            float4v g = *reinterpret_cast<const float4v *>(lds + token * kSumRow32 + c);
+            const float4v u = *reinterpret_cast<const float4v *>(lds + token * kSumRow32 + 16 + c);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) g[i] = silu(g[i]) * u[i];
+            if (token0 + token < count && r < p.tile_rows) store_4<DT>(p, y_at(token0 + token), r / 2 * 16 + c, g);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int token = 8 * j + (lane >> 3), c = 4 * (lane & 7);
+            const float4v y = *reinterpret_cast<const float4v *>(lds + token * kSumRow32 + c);
+            if (token0 + token < count) store_4<DT>(p, y_at(token0 + token), r * 16 + c, y);
+        }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+}
+
+// Few workgroups: the division of the work as above, with X through a part of LDS that each wave has for itself.  A wave's load takes 256 bytes of four rows
+// (the pieces of 32 bytes that the matrix units take are a part of a line each, and the rest is gone from the L1 before it is asked for).  The rows of a
+// step are read into registers at once and those of the next step fetched into their place.
 template <int DT, int CH, bool ZEROS, int MT>
 __global__ void __launch_bounds__(512) q4_mid_kernel(const MmParams p)
 {
-    constexpr int kGroups = 4 / CH, kRows = 16 * MT, NT = 4;
+    constexpr int kGroups = 4 / CH, kRows = 32 * MT;
     extern __shared__ __attribute__((aligned(16))) float sums[];
     __shared__ const char *row_lds[kRows];                             // where the rows of X begin
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n_waves = blockDim.x >> 6, n = lane & 15, q = lane >> 4;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n_waves = blockDim.x >> 6, half = lane >> 5;
     const RowTile rt = row_tile(p, blockIdx.x / p.col_blocks, kRows);
     if (rt.count == 0) return;
-    const SixteenPlus<DT> sixteen_plus;
-    const int64_t last = p.tile_rows - 1, r0 = (int64_t)(blockIdx.x % p.col_blocks) * NT;
-    const int further = (int)(last - r0 < NT ? last - r0 : NT - 1);
-    const int64_t from = rt.mat * p.tile_rows + r0;
-    const char *w_at = reinterpret_cast<const char *>(p.tiles) + from * p.k_tiles * 1024;
-    const char *s_at = p.scales + from * p.steps * (32 * kGroups), *z_at = p.zeros + from * p.steps * (16 * kGroups);
+    const int64_t r0 = (int64_t)(blockIdx.x % p.col_blocks) * 4;
+    // The steps of a wave, begun at another one in every workgroup: rows of X and W are powers of two apart more often than not, and what is read at the
+    // same time should not lie in the same channels.
     const int n_tiles = (int)p.k_tiles, begin = (int)((int64_t)n_tiles * wave / n_waves), n_steps = (int)((int64_t)n_tiles * (wave + 1) / n_waves) - begin;
     const int turn = n_steps > 0 ? (int)(blockIdx.x % p.col_blocks) % n_steps : 0;
-    auto tile_of = [&](int u) {
+    auto tile_of = [&](int u) {                                        // (a wave without steps fetches, too: a tile that is there)
         const int v = (u < n_steps ? u : n_steps > 0 ? n_steps - 1 : 0) + turn, t = begin + (v < n_steps ? v : v - n_steps);
         return t < n_tiles ? t : n_tiles - 1;
     };
-    uint4v w[NT];
-    Words<kGroups> sz[NT];
-    auto fetch_w = [&](int h, int t) {
-        const uint32_t hh = h < further ? h : further;
-        w[h] = *reinterpret_cast<const uint4v *>(w_at + ((hh * (uint32_t)n_tiles + (uint32_t)t) * 1024u + (uint32_t)lane * 16u));
-        const uint32_t at = (hh * (uint32_t)p.steps + (uint32_t)(t / p.tiles_a_step)) * 16u + (uint32_t)n;
-        sz[h].s = *reinterpret_cast<const typename Words<kGroups>::Scales *>(s_at + at * (2u * kGroups));
-        if constexpr (ZEROS) sz[h].z = *reinterpret_cast<const typename Words<kGroups>::Zeros *>(z_at + at * (uint32_t)kGroups);
-    };
+    Pairs<DT, CH, ZEROS, MT> pairs(p, rt.mat, r0, lane);
     // rows behind the last one are the first again, and never stored
     if (threadIdx.x < kRows)
         row_lds[threadIdx.x] = reinterpret_cast<const char *>(p.X + x_row(p, y_row(p, rt.first + ((int)threadIdx.x < rt.count ? threadIdx.x : 0))) * p.ldx);
@@ -442,133 +551,108 @@ __global__ void __launch_bounds__(512) q4_mid_kernel(const MmParams p)
     const uint32_t x_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint4v *)mine_x;
     auto fetch_x = [&](int t) {
         const uint32_t left = (uint32_t)(p.k_chunks - 4 * t) * 4u - 1u;       // the last chunk that is there
-        static_for<4 * MT>([&](auto j) {
-            uint32_t c = (uint32_t)n ^ (uint32_t)(4 * (j.value & 3) + q);
+        static_for<kRows / 4>([&](auto j) {
+            uint32_t c = (uint32_t)(lane & 15) ^ (uint32_t)(4 * (j.value & 3) + (lane >> 4));
             c = c < left ? c : left;
-            const char *src = row_lds[4 * j.value + q] + ((uint32_t)t * 256u + c * 16u);
-            dma16(src, x_base + j.value * 1024);
+            dma16(row_lds[4 * j.value + (lane >> 4)] + ((uint32_t)t * 256u + c * 16u), x_base + j.value * 1024);
         });
     };
     fetch_x(tile_of(0));
-#pragma unroll
-    for (int h = 0; h < NT; ++h) fetch_w(h, tile_of(0));
-    float4v acc[MT][NT];
-    float taken[NT], of_x[MT];                                         // -s (16 + z) and the sum of x of the q-th of four groups
-#pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int h = 0; h < NT; ++h) acc[m][h] = float4v{0, 0, 0, 0};
-#pragma unroll
-    for (int h = 0; h < NT; ++h) taken[h] = 0.f;
+    pairs.fetch(p, 0, tile_of(0));
+    pairs.fetch(p, 1, tile_of(0));
+    float of_x[MT];                                                    // the sum of x in this half's one of two groups
 #pragma unroll
     for (int m = 0; m < MT; ++m) of_x[m] = 0.f;
-    auto take = [&]() {
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-            for (int h = 0; h < NT; ++h) acc[m][h] = __builtin_amdgcn_mfma_f32_16x16x4f32(of_x[m], taken[h], acc[m][h], 0, 0, 0);
-#pragma unroll
-        for (int h = 0; h < NT; ++h) taken[h] = 0.f;
-    };
     for (int u = 0; u < n_steps; ++u) {
         const int t = tile_of(u), next = tile_of(u + 1);
-        // X of this step is there when nothing but the NT loads of codes behind it is on its way (with them go those of scales and zero points)
-        wait_vmcnt<NT>();
-        short8v xf[MT][4];
+        // X of this step is there when nothing but the four loads of codes behind it is on its way (with them go those of scales and zero points)
+        wait_vmcnt<4>();
+        short8v xf[MT][8];
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) xf[m][i] = __builtin_bit_cast(short8v, mine_x[(16 * m + n) * 16 + ((4 * i + q) ^ n)]);
+            for (int i = 0; i < 8; ++i) xf[m][i] = __builtin_bit_cast(short8v, mine_x[(32 * m + (lane & 31)) * 16 + ((2 * i + half) ^ (lane & 15))]);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");             // read before it is written again
         fetch_x(next);
         if (4 * t + 4 > p.k_chunks) {                                  // the last columns are fewer
 #pragma unroll
-            for (int i = 1; i < 4; ++i)
-                if (4 * t + i >= p.k_chunks) {
+            for (int i = 2; i < 8; ++i)
+                if (4 * t + i / 2 >= p.k_chunks) {
 #pragma unroll
                     for (int m = 0; m < MT; ++m) xf[m][i] = short8v{0, 0, 0, 0, 0, 0, 0, 0};
                 }
         }
 #pragma unroll
         for (int g = 0; g < kGroups; ++g) {
-            const int slot = (u * kGroups + g) & 3;
+            const int slot = (CH == 4 ? u : g) & 1;
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
                 float s = 0.f;
 #pragma unroll
-                for (int i = g * CH; i < (g + 1) * CH; ++i) s += sum_of_8<DT>(__builtin_bit_cast(uint4v, xf[m][i]));
-                s = sum_over_quarters(s);
-                of_x[m] = q == slot ? s : of_x[m];
+                for (int i = 2 * CH * g; i < 2 * CH * (g + 1); ++i) s += sum_of_8<DT>(__builtin_bit_cast(uint4v, xf[m][i]));
+                s = sum_over_halves(s);
+                of_x[m] = half == slot ? s : of_x[m];
             }
-#pragma unroll
-            for (int h = 0; h < NT; ++h) {
-                float4v part[MT];
-#pragma unroll
-                for (int m = 0; m < MT; ++m) part[m] = float4v{0, 0, 0, 0};
-#pragma unroll
-                for (int i = g * CH; i < (g + 1) * CH; ++i) {
-                    const short8v b = sixteen_plus(w[h][i]);
-#pragma unroll
-                    for (int m = 0; m < MT; ++m) part[m] = mfma16x16x32<DT>(xf[m][i], b, part[m]);
-                }
-                const float s = sz[h].template scale<DT>(g);
-                if constexpr (CH == 1) {
-                    if (g == 0) taken[h] = sz[h].template scale<DT>(q) * (ZEROS ? sz[h].minus_sixteen_plus_zero(q) : -24.f);
-                } else {
-                    taken[h] = q == slot ? s * (ZEROS ? sz[h].minus_sixteen_plus_zero(g) : -24.f) : taken[h];
-                }
-                if (g == kGroups - 1) fetch_w(h, next);                // a step ahead, into the registers just read
-#pragma unroll
-                for (int m = 0; m < MT; ++m)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[m][h][i] = __builtin_fmaf(s, part[m][i], acc[m][h][i]);
-            }
-            if (g == kGroups - 1 && slot == 3) take();
+            pairs.group(p, g, u, next, u + 1 == n_steps, half, [&](int m, int i) { return xf[m][i]; }, [&](int m, int) { return of_x[m]; });
             __builtin_amdgcn_sched_barrier(0);
         }
     }
-    if constexpr (CH > 1) take();                                      // what is left of four groups; of the others taken is zero
     // The waves' sums are added pairwise from the back: half of them write, the other half adds, until one is left.
     wait_vmcnt<0>();                                                   // (the last step fetched its own again)
     __syncthreads();
-    for (int half = n_waves >> 1; half > 0; half >>= 1) {
-        float *place = sums + (int64_t)(wave - half) * NT * kRows * kSumRow;
-        if (wave >= half && wave < 2 * half) {
+    for (int rest = n_waves >> 1; rest > 0; rest >>= 1) {
+        float4v *place = reinterpret_cast<float4v *>(sums) + (int64_t)(wave % rest) * (MT * 2 * 4 * 64) + lane;
+        if (wave >= rest && wave < 2 * rest) {
 #pragma unroll
             for (int m = 0; m < MT; ++m)
 #pragma unroll
-                for (int h = 0; h < NT; ++h)
+                for (int h = 0; h < 2; ++h)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) place[(h * kRows + 16 * m + 4 * q + i) * kSumRow + n] = acc[m][h][i];
+                    for (int i = 0; i < 4; ++i)
+                        place[((m * 2 + h) * 4 + i) * 64] = float4v{pairs.acc[m][h][4 * i], pairs.acc[m][h][4 * i + 1], pairs.acc[m][h][4 * i + 2], pairs.acc[m][h][4 * i + 3]};
         }
         __syncthreads();
-        if (wave < half) {
-            const float *theirs = sums + (int64_t)wave * NT * kRows * kSumRow;
+        if (wave < rest) {
 #pragma unroll
             for (int m = 0; m < MT; ++m)
 #pragma unroll
-                for (int h = 0; h < NT; ++h)
+                for (int h = 0; h < 2; ++h)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[m][h][i] += theirs[(h * kRows + 16 * m + 4 * q + i) * kSumRow + n];
+                    for (int i = 0; i < 4; ++i) {
+                        const float4v o = place[((m * 2 + h) * 4 + i) * 64];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) pairs.acc[m][h][4 * i + j] += o[j];
+                    }
         }
         __syncthreads();
     }
+    // the first wave has them all: it hands every wave a share to store
     if (wave == 0) {
+        float4v *place = reinterpret_cast<float4v *>(sums) + lane;
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
-            for (int h = 0; h < NT; ++h)
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) sums[(h * kRows + 16 * m + 4 * q + i) * kSumRow + n] = acc[m][h][i];
+                for (int i = 0; i < 4; ++i)
+                    place[((m * 2 + h) * 4 + i) * 64] = float4v{pairs.acc[m][h][4 * i], pairs.acc[m][h][4 * i + 1], pairs.acc[m][h][4 * i + 2], pairs.acc[m][h][4 * i + 3]};
     }
     __syncthreads();
-    store_sums<DT, NT, kRows>(p, rt, r0, sums, 1);
+    float *own = sums + MT * 2 * 1024 + wave * (32 * kSumRow32);
+    for (int part = wave; part < MT * 2; part += n_waves) {
+        float16v v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float4v o = reinterpret_cast<const float4v *>(sums)[(part * 4 + i) * 64 + lane];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[4 * i + j] = o[j];
+        }
+        store_32<DT>(p, rt.count, part / 2 * 32, r0 + part % 2 * 2, own, v, lane, [&](int token) { return y_row(p, rt.first + token) * p.ldy; });
+    }
 }
 
-// ---- many rows: 16 MT of them times 16 rows of tiles, by four waves with four rows of tiles each.  A step is a tile's 128 columns: X goes through LDS,
-// which all waves read; W comes straight into registers, as it was laid out, and is turned into numbers there.
-constexpr int kManyRows = 4;           // rows of tiles a wave
-
+// Many workgroups: 32 MT rows of X times 16 rows of tiles, by four waves with four rows of tiles each.  X goes through LDS, which all waves read; W
+// comes straight into registers, as it was laid out, and is turned into numbers there.
 template <int CTRL>
 __device__ __forceinline__ float add_lane(float x)
 {
@@ -578,75 +662,48 @@ __device__ __forceinline__ float add_lane(float x)
 template <int DT, int CH, bool ZEROS, int MT>
 __global__ void __launch_bounds__(256, 2) q4_many_kernel(const MmParams p)
 {
-    constexpr int kRows = 16 * MT, kGroups = 4 / CH, NT = kManyRows;
-    __shared__ __attribute__((aligned(16))) uint4v x_lds[2][kRows * 16];         // chunk c of row r at r * 16 + (c ^ r % 16)
-    __shared__ float sum_lds[2][4][kRows];                                       // of four groups in turn
+    constexpr int kRows = 32 * MT, kGroups = 4 / CH, kSums = CH == 1 ? 8 : 4, kLoads = kRows / 16;
+    constexpr int kXBytes = 2 * kRows * 256, kOutBytes = 4 * 32 * kSumRow32 * 4;
+    __shared__ __attribute__((aligned(16))) char lds[kXBytes > kOutBytes ? kXBytes : kOutBytes];
+    __shared__ float sum_lds[kSums][kRows];                                      // of the groups of two tiles, or of four tiles
     __shared__ int64_t y_lds[kRows];                                             // where the rows of Y begin
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, q = lane >> 4;
+    uint4v(*x_lds)[kRows * 16] = reinterpret_cast<uint4v(*)[kRows * 16]>(lds);   // chunk c of row r at r * 16 + (c ^ r % 16)
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     const RowTile rt = row_tile(p, blockIdx.x / p.col_blocks, kRows);
     if (rt.count == 0) return;
-    const SixteenPlus<DT> sixteen_plus;
-    const int64_t last = p.tile_rows - 1, r0 = ((int64_t)(blockIdx.x % p.col_blocks) * 4 + wave) * NT;
-    // W from the wave's first row of tiles on (behind the last one, that one), 32-bit offsets from there
-    const int64_t from = rt.mat * p.tile_rows + (r0 < last ? r0 : last);
-    const int further = (int)(last - r0 < 0 ? 0 : last - r0 < NT ? last - r0 : NT - 1);
-    const char *w_at = reinterpret_cast<const char *>(p.tiles) + from * p.k_tiles * 1024;
-    const char *s_at = p.scales + from * p.steps * (32 * kGroups), *z_at = p.zeros + from * p.steps * (16 * kGroups);
-    uint32_t w_row[NT], s_row[NT];
-#pragma unroll
-    for (int h = 0; h < NT; ++h) {
-        w_row[h] = (uint32_t)((h < further ? h : further) * p.k_tiles) * 1024u;
-        s_row[h] = (uint32_t)((h < further ? h : further) * p.steps) * 16u;
-    }
-
-    uint4v w[NT];
-    Words<kGroups> sz[NT];
-    auto fetch_w = [&](int h, int t) {
-        w[h] = *reinterpret_cast<const uint4v *>(w_at + (w_row[h] + (uint32_t)t * 1024u + (uint32_t)lane * 16u));
-        const uint32_t at = s_row[h] + (uint32_t)(t / p.tiles_a_step) * 16u + (uint32_t)n;
-        sz[h].s = *reinterpret_cast<const typename Words<kGroups>::Scales *>(s_at + at * (2u * kGroups));
-        if constexpr (ZEROS) sz[h].z = *reinterpret_cast<const typename Words<kGroups>::Zeros *>(z_at + at * (uint32_t)kGroups);
-    };
-#pragma unroll
-    for (int h = 0; h < NT; ++h) fetch_w(h, 0);
+    const int64_t r0 = ((int64_t)(blockIdx.x % p.col_blocks) * 4 + wave) * 4;
+    Pairs<DT, CH, ZEROS, MT> pairs(p, rt.mat, r0, lane);
+    pairs.fetch(p, 0, 0);
+    pairs.fetch(p, 1, 0);
 
     // this thread's chunks of X: chunk c of rows xr + 16 j
     const int c = threadIdx.x & 15, xr = threadIdx.x >> 4;
-    const uint16_t *src[MT];
+    const uint16_t *src[kLoads];
 #pragma unroll
-    for (int j = 0; j < MT; ++j) {
+    for (int j = 0; j < kLoads; ++j) {
         const int64_t row = y_row(p, rt.first + (xr + 16 * j < rt.count ? xr + 16 * j : 0));
         if (c == 0) y_lds[xr + 16 * j] = row * p.ldy;
         src[j] = p.X + x_row(p, row) * p.ldx + 8 * c;
     }
-    uint4v xv[MT];
+    uint4v xv[kLoads];
     auto fetch_x = [&](int t) {
 #pragma unroll
-        for (int j = 0; j < MT; ++j) {
+        for (int j = 0; j < kLoads; ++j) {
             xv[j] = uint4v{0, 0, 0, 0};
             if (4 * t + (c >> 2) < p.k_chunks) xv[j] = *reinterpret_cast<const uint4v *>(src[j] + 128 * (int64_t)t);
         }
     };
     auto put_x = [&](int t) {
 #pragma unroll
-        for (int j = 0; j < MT; ++j) {
+        for (int j = 0; j < kLoads; ++j) {
             x_lds[t & 1][(xr + 16 * j) * 16 + (c ^ (xr & 15))] = xv[j];
             float s = sum_of_8<DT>(xv[j]);
             s = add_lane<0x4E>(add_lane<0xB1>(s));            // over four lanes, then eight, then sixteen
             if constexpr (CH >= 2) s = add_lane<0x141>(s);
             if constexpr (CH == 4) s = add_lane<0x140>(s);
-            const int g = t * kGroups + c / (4 * CH);
-            if (c % (4 * CH) == 0) sum_lds[g >> 2 & 1][g & 3][xr + 16 * j] = s;
+            if (c % (4 * CH) == 0) sum_lds[(t * kGroups + c / (4 * CH)) % kSums][xr + 16 * j] = s;
         }
     };
-    float4v acc[MT][NT];
-#pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int h = 0; h < NT; ++h) acc[m][h] = float4v{0, 0, 0, 0};
-    float taken[NT];                                              // -s (16 + z) of the q-th of four groups
-#pragma unroll
-    for (int h = 0; h < NT; ++h) taken[h] = 0.f;
     const int n_tiles = (int)p.k_tiles;
     fetch_x(0);
     put_x(0);
@@ -656,72 +713,23 @@ __global__ void __launch_bounds__(256, 2) q4_many_kernel(const MmParams p)
         fetch_x(next);
 #pragma unroll
         for (int g = 0; g < kGroups; ++g) {
-            const int slot = (t * kGroups + g) & 3;
-            short8v xf[MT][CH];
+            short8v xf[MT][2 * CH];
 #pragma unroll
             for (int m = 0; m < MT; ++m)
 #pragma unroll
-                for (int i = 0; i < CH; ++i) xf[m][i] = __builtin_bit_cast(short8v, x_lds[t & 1][(16 * m + n) * 16 + ((4 * (g * CH + i) + q) ^ n)]);
-#pragma unroll
-            for (int h = 0; h < NT; ++h) {
-                float4v part[MT];
-#pragma unroll
-                for (int m = 0; m < MT; ++m) part[m] = float4v{0, 0, 0, 0};
-#pragma unroll
-                for (int i = 0; i < CH; ++i) {
-                    const short8v b = sixteen_plus(w[h][g * CH + i]);
-#pragma unroll
-                    for (int m = 0; m < MT; ++m) part[m] = mfma16x16x32<DT>(xf[m][i], b, part[m]);
-                }
-                const float s = sz[h].template scale<DT>(g);
-                if constexpr (CH == 1) {
-                    if (g == 0) taken[h] = sz[h].template scale<DT>(q) * (ZEROS ? sz[h].minus_sixteen_plus_zero(q) : -24.f);
-                } else {
-                    taken[h] = q == slot ? s * (ZEROS ? sz[h].minus_sixteen_plus_zero(g) : -24.f) : taken[h];
-                }
-                if (g == kGroups - 1) fetch_w(h, next);           // a step ahead, into the registers just read
-#pragma unroll
-                for (int m = 0; m < MT; ++m)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[m][h][i] = __builtin_fmaf(s, part[m][i], acc[m][h][i]);
-            }
-            if (g == kGroups - 1 && (slot == 3 || t + 1 == n_tiles)) {
-                const int four = (t * kGroups + g) >> 2 & 1;
-#pragma unroll
-                for (int m = 0; m < MT; ++m) {
-                    const float of_x = q <= slot ? sum_lds[four][q][16 * m + n] : 0.f;
-#pragma unroll
-                    for (int h = 0; h < NT; ++h) acc[m][h] = __builtin_amdgcn_mfma_f32_16x16x4f32(of_x, taken[h], acc[m][h], 0, 0, 0);
-                }
-#pragma unroll
-                for (int h = 0; h < NT; ++h) taken[h] = 0.f;
-            }
+                for (int i = 0; i < 2 * CH; ++i) xf[m][i] = __builtin_bit_cast(short8v, x_lds[t & 1][(32 * m + (lane & 31)) * 16 + ((2 * (g * 2 * CH + i) + half) ^ (lane & 15))]);
+            pairs.group(p, g, t, next, t + 1 == n_tiles, half, [&](int m, int i) { return xf[m][i - g * 2 * CH]; },
+                        [&](int m, int g) { return sum_lds[((CH == 4 ? t & ~1 : t * kGroups + g - 1) + half) % kSums][32 * m + (lane & 31)]; });
             __builtin_amdgcn_sched_barrier(0);                    // (groups taken up at once take registers that are not there)
         }
         if (t + 1 < n_tiles) put_x(t + 1);
         __syncthreads();
     }
+    float *own = reinterpret_cast<float *>(lds) + wave * (32 * kSumRow32);
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int token = 16 * m + 4 * q + i;
-            if (token >= rt.count) continue;
-            const int64_t at = y_lds[token];
-            if (p.gated) {
-#pragma unroll
-                for (int h = 0; h < NT; h += 2) {
-                    const int64_t col = (r0 + h) / 2 * 16 + n;
-                    if (r0 + h < last && col < p.half) store_y<DT>(p, at + col, silu(acc[m][h][i]) * acc[m][h + 1][i]);
-                }
-            } else {
-#pragma unroll
-                for (int h = 0; h < NT; ++h) {
-                    const int64_t col = (r0 + h) * 16 + n;
-                    if (col < p.half) store_y<DT>(p, at + col, acc[m][h][i]);
-                }
-            }
-        }
+        for (int h = 0; h < 2; ++h) store_32<DT>(p, rt.count, 32 * m, r0 + 2 * h, own, pairs.acc[m][h], lane, [&](int token) { return y_lds[token]; });
 }
 
 using MmKernel = void (*)(MmParams);
@@ -734,18 +742,20 @@ Variant split_variant(int waves)
 {
     return {q4_split_kernel<DT, CH, ZEROS, MT, NT, AHEAD_W, AHEAD_X, THREADS>, 16 * MT, NT, 64 * waves, waves * NT * 16 * MT * kSumRow * 4};
 }
+template <int DT, int CH, bool ZEROS, int MT>
+Variant mid_variant(int waves)
+{
+    const int x = waves * 32 * MT * 256, halves = waves / 2 * MT * 2 * 4096, out = MT * 2 * 4096 + waves * 32 * kSumRow32 * 4;
+    return {q4_mid_kernel<DT, CH, ZEROS, MT>, 32 * MT, 4, 64 * waves, std::max(x, std::max(halves, out))};
+}
 template <int DT, int CH, bool ZEROS>
 Variant mm_variant(int32_t rows, int split, int waves)
 {
     if (rows == 16 && split == 1) return split_variant<DT, CH, ZEROS, 1, 1, 4, 2, 1024>(waves);
     if (rows == 16 && split == 2) return split_variant<DT, CH, ZEROS, 1, 2, 4, 2, 1024>(waves);
     if (rows == 16) return split_variant<DT, CH, ZEROS, 1, 4, 2, 2, 512>(waves);
-    if (rows == 32 && split == 2) return {q4_mid_kernel<DT, CH, ZEROS, 2>, 32, 4, 64 * waves, waves * 2 * 4096 > waves / 2 * 4 * 32 * kSumRow * 4 ? waves * 2 * 4096 : waves / 2 * 4 * 32 * kSumRow * 4};
-    if (rows == 64 && split == 2) return {q4_mid_kernel<DT, CH, ZEROS, 4>, 64, 4, 64 * waves, waves * 4 * 4096 > waves / 2 * 4 * 64 * kSumRow * 4 ? waves * 4 * 4096 : waves / 2 * 4 * 64 * kSumRow * 4};
-    if (rows == 32 && split) return split_variant<DT, CH, ZEROS, 2, 4, 1, 1, 512>(waves);
-    if (rows == 32) return {q4_many_kernel<DT, CH, ZEROS, 2>, 32, 4 * kManyRows, 256, 0};
-    if (split) return split_variant<DT, CH, ZEROS, 4, 4, 1, 1, 512>(waves);
-    return {q4_many_kernel<DT, CH, ZEROS, 4>, 64, 4 * kManyRows, 256, 0};
+    if (split) return rows == 32 ? mid_variant<DT, CH, ZEROS, 1>(waves) : mid_variant<DT, CH, ZEROS, 2>(waves);
+    return rows == 32 ? Variant{q4_many_kernel<DT, CH, ZEROS, 1>, 32, 16, 256, 0} : Variant{q4_many_kernel<DT, CH, ZEROS, 2>, 64, 16, 256, 0};
 }
 template <int DT>
 Variant mm_variant(int32_t group, bool zeros, int32_t rows, int split, int waves)
