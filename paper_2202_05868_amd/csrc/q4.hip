@@ -90,6 +90,19 @@ __global__ void __launch_bounds__(256) q4_pack_scales_kernel(const PackParams p)
 }
 
 // ---- the products
+
+// i / d for i below 2^31: 2^(31 + l) / d rounded up, l the bits of d - 1, times i
+struct Divide {
+    uint32_t factor;
+    int32_t shift;
+    static Divide by(int64_t d)
+    {
+        const int l = d > 1 ? 64 - __builtin_clzll((unsigned long long)d - 1) : 0;
+        return {(uint32_t)(((1ull << (31 + l)) + d - 1) / d), 31 + l};
+    }
+    __device__ __forceinline__ uint32_t operator()(uint32_t i) const { return (uint32_t)((uint64_t)i * factor >> shift); }
+};
+
 struct MmParams {
     const uint4v *tiles;
     const char *scales, *zeros;
@@ -97,14 +110,16 @@ struct MmParams {
     void *Y;
     int64_t ldx, ldy, n_rows;                  // rows of Y
     int64_t k_tiles, tile_rows, steps;
-    int32_t half, k_chunks, tiles_a_step;      // k_chunks: columns / 32
+    uint32_t x_bytes, ldx_bytes;               // of X from its first element to its last; of a row to the next; 0 where that is beyond 32 bits
+    int32_t half, k_chunks, lg_waves;          // k_chunks: columns / 32; lg_waves: of the waves of a workgroup that share the columns
+    uint32_t step_divide;                      // tile t is of step t, or t step_divide >> 32 where that is not zero
     int32_t gated, f32, fours;                 // fours: four elements of Y from a multiple of four on are aligned to as much
-    int32_t col_blocks, row_tiles;             // of the launch; row_tiles: at most so many, if routed
+    int32_t col_blocks;                        // of the launch: workgroup i has tile of rows i / col_blocks
+    Divide by_col_blocks;
     // routed, or null
     const PlanTile *plan_tiles;
     const int32_t *order;
-    uint32_t divide;                           // the row of X of pair i is i divide >> divide_shift
-    int32_t divide_shift;
+    Divide by_places;                          // the pairs of a row of X
 };
 
 template <int DT>
@@ -206,7 +221,25 @@ __device__ __forceinline__ RowTile row_tile(const MmParams &p, int tile, int row
     const int64_t first = (int64_t)tile * rows, left = p.n_rows - first;
     return {0, first, (int32_t)(left < rows ? left : rows)};
 }
-__device__ __forceinline__ int64_t x_row(const MmParams &p, int64_t y_row) { return p.order ? (int64_t)((uint64_t)y_row * p.divide >> p.divide_shift) : y_row; }
+__device__ __forceinline__ int64_t x_row(const MmParams &p, int64_t y_row) { return p.order ? (int64_t)p.by_places((uint32_t)y_row) : y_row; }
+__device__ __forceinline__ uint32_t step_of(const MmParams &p, int t) { return p.step_divide ? __umulhi((uint32_t)t, p.step_divide) : (uint32_t)t; }
+
+// The steps of a wave among those that share the columns, begun at another one in every workgroup: rows of X and W are powers of two apart more often than
+// not, and what is read at the same time should not lie in the same channels.
+struct Steps {
+    int begin, count, turn, n_tiles;
+    __device__ __forceinline__ Steps(const MmParams &p, int wave, uint32_t workgroup) : n_tiles((int)p.k_tiles)
+    {
+        begin = n_tiles * wave >> p.lg_waves;
+        count = (n_tiles * (wave + 1) >> p.lg_waves) - begin;
+        turn = (int)((workgroup * 40503u & 0xFFFFu) * (uint32_t)count >> 16);
+    }
+    __device__ __forceinline__ int operator()(int u) const        // the tile of step u; behind the last one that one; without any, one that is there
+    {
+        const int v = (u < count ? u : count > 0 ? count - 1 : 0) + turn, t = begin + (v < count ? v : v - count);
+        return t < n_tiles ? t : n_tiles - 1;
+    }
+};
 __device__ __forceinline__ int64_t y_row(const MmParams &p, int64_t at) { return p.order ? p.order[at] : at; }
 
 typedef _Float16 half2v __attribute__((ext_vector_type(2)));
@@ -274,23 +307,18 @@ __global__ void __launch_bounds__(THREADS) q4_split_kernel(const MmParams p)
 {
     constexpr int kGroups = 4 / CH, kRows = 16 * MT;
     extern __shared__ __attribute__((aligned(16))) float sums[];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n_waves = blockDim.x >> 6, n = lane & 15, q = lane >> 4;
-    const RowTile rt = row_tile(p, blockIdx.x / p.col_blocks, kRows);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n_waves = 1 << p.lg_waves, n = lane & 15, q = lane >> 4;
+    const uint32_t tile = p.by_col_blocks(blockIdx.x), col_block = blockIdx.x - tile * p.col_blocks;
+    const RowTile rt = row_tile(p, tile, kRows);
     if (rt.count == 0) return;
     const SixteenPlus<DT> sixteen_plus;
-    const int64_t last = p.tile_rows - 1, r0 = (int64_t)(blockIdx.x % p.col_blocks) * NT;
+    const int64_t last = p.tile_rows - 1, r0 = (int64_t)col_block * NT;
     const int further = (int)(last - r0 < NT ? last - r0 : NT - 1);
     const int64_t from = rt.mat * p.tile_rows + r0;
     const char *w_at = reinterpret_cast<const char *>(p.tiles) + from * p.k_tiles * 1024;
     const char *s_at = p.scales + from * p.steps * (32 * kGroups), *z_at = p.zeros + from * p.steps * (16 * kGroups);
-    // The steps of a wave, begun at another one in every workgroup: rows of X and W are powers of two apart more often than not, and what is read at the
-    // same time should not lie in the same channels.
-    const int n_tiles = (int)p.k_tiles, begin = (int)((int64_t)n_tiles * wave / n_waves), n_steps = (int)((int64_t)n_tiles * (wave + 1) / n_waves) - begin;
-    const int turn = n_steps > 0 ? (int)(blockIdx.x % p.col_blocks) % n_steps : 0;
-    auto tile_of = [&](int u) {                                        // (a wave without steps fetches, too: a tile that is there)
-        const int v = (u < n_steps ? u : n_steps > 0 ? n_steps - 1 : 0) + turn, t = begin + (v < n_steps ? v : v - n_steps);
-        return t < n_tiles ? t : n_tiles - 1;
-    };
+    const Steps tile_of(p, wave, col_block);
+    const int n_tiles = tile_of.n_tiles, n_steps = tile_of.count;
 
     uint4v w[AHEAD_W][NT];
     Words<kGroups> sz[AHEAD_W][NT];
@@ -298,7 +326,7 @@ __global__ void __launch_bounds__(THREADS) q4_split_kernel(const MmParams p)
     auto fetch_w = [&](auto d, int h, int t) {
         const uint32_t hh = h < further ? h : further;
         w[d][h] = *reinterpret_cast<const uint4v *>(w_at + ((hh * (uint32_t)n_tiles + (uint32_t)t) * 1024u + (uint32_t)lane * 16u));
-        const uint32_t at = (hh * (uint32_t)p.steps + (uint32_t)(t / p.tiles_a_step)) * 16u + (uint32_t)n;
+        const uint32_t at = (hh * (uint32_t)p.steps + step_of(p, t)) * 16u + (uint32_t)n;
         sz[d][h].s = *reinterpret_cast<const typename Words<kGroups>::Scales *>(s_at + at * (2u * kGroups));
         if constexpr (ZEROS) sz[d][h].z = *reinterpret_cast<const typename Words<kGroups>::Zeros *>(z_at + at * (uint32_t)kGroups);
     };
@@ -306,16 +334,18 @@ __global__ void __launch_bounds__(THREADS) q4_split_kernel(const MmParams p)
 #pragma unroll
         for (int h = 0; h < NT; ++h) fetch_w(d, h, tile_of(d));
     });
-    // rows behind the last one are that of the first again, and never stored
-    const uint16_t *x[MT];
+    // Rows behind the last one are out of X's range: loads of them cost nothing.
+    const __amdgpu_buffer_rsrc_t x_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(p.X), 0, (int)p.x_bytes, 0x00020000);
+    uint32_t x_at[MT];
 #pragma unroll
-    for (int m = 0; m < MT; ++m) x[m] = p.X + x_row(p, y_row(p, rt.first + (16 * m + n < rt.count ? 16 * m + n : 0))) * p.ldx + 8 * q;
+    for (int m = 0; m < MT; ++m)
+        x_at[m] = 16 * m + n < rt.count ? (uint32_t)x_row(p, y_row(p, rt.first + 16 * m + n)) * p.ldx_bytes + 16 * q : 0xFFFFF000u;
     auto fetch_x = [&](auto d, int t) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int chunk = 4 * t + i < p.k_chunks ? 4 * t + i : p.k_chunks - 1;
 #pragma unroll
-            for (int m = 0; m < MT; ++m) xf[d][m][i] = *reinterpret_cast<const short8v *>(x[m] + 32 * (int64_t)chunk);
+            for (int m = 0; m < MT; ++m) xf[d][m][i] = __builtin_bit_cast(short8v, __builtin_amdgcn_raw_buffer_load_b128(x_rsrc, (int)x_at[m], 64 * chunk, 0));
         }
     };
     static_for<AHEAD_X>([&](auto d) { fetch_x(d, tile_of(d)); });
@@ -449,7 +479,7 @@ struct Pairs {
     {
         w[h][0] = *reinterpret_cast<const uint4v *>(w_at[h] + (uint32_t)t * 1024u);
         w[h][1] = *reinterpret_cast<const uint4v *>(w_at[h] + (uint32_t)t * 1024u + 512);
-        const uint32_t step = (uint32_t)(t / p.tiles_a_step);
+        const uint32_t step = step_of(p, t);
         sz[h].s = *reinterpret_cast<const typename Words<kGroups>::Scales *>(s_at[h] + step * (32u * kGroups));
         if constexpr (ZEROS) sz[h].z = *reinterpret_cast<const typename Words<kGroups>::Zeros *>(z_at[h] + step * (16u * kGroups));
     }
@@ -529,18 +559,13 @@ __global__ void __launch_bounds__(512) q4_mid_kernel(const MmParams p)
     constexpr int kGroups = 4 / CH, kRows = 32 * MT;
     extern __shared__ __attribute__((aligned(16))) float sums[];
     __shared__ const char *row_lds[kRows];                             // where the rows of X begin
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n_waves = blockDim.x >> 6, half = lane >> 5;
-    const RowTile rt = row_tile(p, blockIdx.x / p.col_blocks, kRows);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n_waves = 1 << p.lg_waves, half = lane >> 5;
+    const uint32_t tile = p.by_col_blocks(blockIdx.x), col_block = blockIdx.x - tile * p.col_blocks;
+    const RowTile rt = row_tile(p, tile, kRows);
     if (rt.count == 0) return;
-    const int64_t r0 = (int64_t)(blockIdx.x % p.col_blocks) * 4;
-    // The steps of a wave, begun at another one in every workgroup: rows of X and W are powers of two apart more often than not, and what is read at the
-    // same time should not lie in the same channels.
-    const int n_tiles = (int)p.k_tiles, begin = (int)((int64_t)n_tiles * wave / n_waves), n_steps = (int)((int64_t)n_tiles * (wave + 1) / n_waves) - begin;
-    const int turn = n_steps > 0 ? (int)(blockIdx.x % p.col_blocks) % n_steps : 0;
-    auto tile_of = [&](int u) {                                        // (a wave without steps fetches, too: a tile that is there)
-        const int v = (u < n_steps ? u : n_steps > 0 ? n_steps - 1 : 0) + turn, t = begin + (v < n_steps ? v : v - n_steps);
-        return t < n_tiles ? t : n_tiles - 1;
-    };
+    const int64_t r0 = (int64_t)col_block * 4;
+    const Steps tile_of(p, wave, col_block);
+    const int n_steps = tile_of.count;
     Pairs<DT, CH, ZEROS, MT> pairs(p, rt.mat, r0, lane);
     // rows behind the last one are the first again, and never stored
     if (threadIdx.x < kRows)
@@ -669,9 +694,10 @@ __global__ void __launch_bounds__(256, 2) q4_many_kernel(const MmParams p)
     __shared__ int64_t y_lds[kRows];                                             // where the rows of Y begin
     uint4v(*x_lds)[kRows * 16] = reinterpret_cast<uint4v(*)[kRows * 16]>(lds);   // chunk c of row r at r * 16 + (c ^ r % 16)
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
-    const RowTile rt = row_tile(p, blockIdx.x / p.col_blocks, kRows);
+    const uint32_t tile = p.by_col_blocks(blockIdx.x), col_block = blockIdx.x - tile * p.col_blocks;
+    const RowTile rt = row_tile(p, tile, kRows);
     if (rt.count == 0) return;
-    const int64_t r0 = ((int64_t)(blockIdx.x % p.col_blocks) * 4 + wave) * 4;
+    const int64_t r0 = ((int64_t)col_block * 4 + wave) * 4;
     Pairs<DT, CH, ZEROS, MT> pairs(p, rt.mat, r0, lane);
     pairs.fetch(p, 0, 0);
     pairs.fetch(p, 1, 0);
@@ -737,10 +763,10 @@ struct Variant {
     MmKernel kernel;
     int32_t rows, tile_rows, threads, lds;             // of a workgroup
 };
-template <int DT, int CH, bool ZEROS, int MT, int NT, int AHEAD_W, int AHEAD_X, int THREADS>
+template <int DT, int CH, bool ZEROS, int NT, int AHEAD_W, int AHEAD_X, int THREADS>
 Variant split_variant(int waves)
 {
-    return {q4_split_kernel<DT, CH, ZEROS, MT, NT, AHEAD_W, AHEAD_X, THREADS>, 16 * MT, NT, 64 * waves, waves * NT * 16 * MT * kSumRow * 4};
+    return {q4_split_kernel<DT, CH, ZEROS, 1, NT, AHEAD_W, AHEAD_X, THREADS>, 16, NT, 64 * waves, waves * NT * 16 * kSumRow * 4};
 }
 template <int DT, int CH, bool ZEROS, int MT>
 Variant mid_variant(int waves)
@@ -748,21 +774,47 @@ Variant mid_variant(int waves)
     const int x = waves * 32 * MT * 256, halves = waves / 2 * MT * 2 * 4096, out = MT * 2 * 4096 + waves * 32 * kSumRow32 * 4;
     return {q4_mid_kernel<DT, CH, ZEROS, MT>, 32 * MT, 4, 64 * waves, std::max(x, std::max(halves, out))};
 }
+
+// The variant for `rows` rows of a tile of rows (16, 32 or 64).
+struct Choice {
+    int32_t rows, nt, waves;                           // nt: rows of tiles of a workgroup; 16: the kernel for many workgroups
+    bool few_steps = false;                            // 16 rows: nothing but the next step fetched ahead, and eight waves a SIMD
+};
 template <int DT, int CH, bool ZEROS>
-Variant mm_variant(int32_t rows, int split, int waves)
+Variant mm_variant(const Choice &c)
 {
-    if (rows == 16 && split == 1) return split_variant<DT, CH, ZEROS, 1, 1, 4, 2, 1024>(waves);
-    if (rows == 16 && split == 2) return split_variant<DT, CH, ZEROS, 1, 2, 4, 2, 1024>(waves);
-    if (rows == 16) return split_variant<DT, CH, ZEROS, 1, 4, 2, 2, 512>(waves);
-    if (split) return rows == 32 ? mid_variant<DT, CH, ZEROS, 1>(waves) : mid_variant<DT, CH, ZEROS, 2>(waves);
-    return rows == 32 ? Variant{q4_many_kernel<DT, CH, ZEROS, 1>, 32, 16, 256, 0} : Variant{q4_many_kernel<DT, CH, ZEROS, 2>, 64, 16, 256, 0};
+    if (c.rows == 16 && c.few_steps) return split_variant<DT, CH, ZEROS, 2, 1, 1, 256>(4);
+    if (c.rows == 16) return c.nt == 1 ? split_variant<DT, CH, ZEROS, 1, 4, 2, 1024>(c.waves) : c.nt == 2 ? split_variant<DT, CH, ZEROS, 2, 4, 2, 1024>(c.waves) : split_variant<DT, CH, ZEROS, 4, 2, 2, 512>(c.waves);
+    if (c.nt == 4) return c.rows == 32 ? mid_variant<DT, CH, ZEROS, 1>(c.waves) : mid_variant<DT, CH, ZEROS, 2>(c.waves);
+    return c.rows == 32 ? Variant{q4_many_kernel<DT, CH, ZEROS, 1>, 32, 16, 256, 0} : Variant{q4_many_kernel<DT, CH, ZEROS, 2>, 64, 16, 256, 0};
 }
 template <int DT>
-Variant mm_variant(int32_t group, bool zeros, int32_t rows, int split, int waves)
+Variant mm_variant(int32_t group, bool zeros, const Choice &c)
 {
-    if (group == 32) return zeros ? mm_variant<DT, 1, true>(rows, split, waves) : mm_variant<DT, 1, false>(rows, split, waves);
-    if (group == 64) return zeros ? mm_variant<DT, 2, true>(rows, split, waves) : mm_variant<DT, 2, false>(rows, split, waves);
-    return zeros ? mm_variant<DT, 4, true>(rows, split, waves) : mm_variant<DT, 4, false>(rows, split, waves);
+    if (group == 32) return zeros ? mm_variant<DT, 1, true>(c) : mm_variant<DT, 1, false>(c);
+    if (group == 64) return zeros ? mm_variant<DT, 2, true>(c) : mm_variant<DT, 2, false>(c);
+    return zeros ? mm_variant<DT, 4, true>(c) : mm_variant<DT, 4, false>(c);
+}
+
+// By how many workgroups there would be for the 256 compute units, in us (bf16, groups of 128, T rows times K x N):
+//   more than 16 rows: the kernel for many workgroups from 224 of them on (T 512, 4096 x 8192, 256 workgroups: 49, the other 55; T 192, 4096 x 14336, 168: 50 and
+//   46; T 256, 4096 x 8192, 128: 48 and 32); the other one with eight waves where a CU has one workgroup and each wave two steps (T 64, 8192 x 16384, 256
+//   workgroups: 34, with four 42; T 256, 4096 x 8192, 512: 39 and 32; T 57, 704 x 12878: 10.7 and 10.0)
+//   up to 16 rows: one row of tiles a workgroup while that is one for each CU (T 1, 4096 x 4096: 6.0, two 6.7; T 1, 8192 x 16384: 20.3 and 17.4), four for as
+//   many as two a CU and more rows of X than four, whose loads then cost (T 16, 8192 x 16384: 19.8, two 23.3; T 1: 19.2 and 17.4).  Where waves have up to four
+//   steps and there are two workgroups for each CU, they hide each other's waits better than loads far ahead do, which take registers (112 pairs of 28
+//   experts, 576 x 1024: 5.5, loads ahead 7.8; 64 pairs of 64 experts, 2048 x 2816: 30.6 and 31.8)
+Choice choose(const MmParams &p, int32_t rows, int64_t row_tiles, int64_t rows_each)
+{
+    const int64_t tiles = row_tiles * p.tile_rows;
+    if (rows > 16) {
+        if (row_tiles * ((p.tile_rows + 15) / 16) >= 224) return {rows, 16, 4};
+        return {rows, 4, row_tiles * ((p.tile_rows + 3) / 4) <= 256 && p.k_tiles >= 16 ? 8 : 4};
+    }
+    if (tiles <= 256 && !p.gated) return {16, 1, p.k_tiles >= 32 ? 8 : 4};
+    if (p.k_tiles <= 16 && tiles >= 1024) return {16, 2, 4, true};
+    if (tiles >= 512 && rows_each > 4) return {16, 4, p.k_tiles >= 16 ? 8 : 4};
+    return {16, 2, 4};
 }
 
 bool aligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
@@ -787,7 +839,7 @@ int mm_args(const q4_t *h, const void *X_dev, int64_t ldx, const void *Y_dev, in
     return VBR_OK;
 }
 
-MmParams mm_params(const q4_t *h, const void *X_dev, int64_t ldx, void *Y_dev, int64_t ldy, int64_t n_rows)
+MmParams mm_params(const q4_t *h, const void *X_dev, int64_t ldx, int64_t x_rows, void *Y_dev, int64_t ldy, int64_t n_rows)
 {
     MmParams p{};
     const char *d = static_cast<const char *>(h->dev);
@@ -798,13 +850,17 @@ MmParams mm_params(const q4_t *h, const void *X_dev, int64_t ldx, void *Y_dev, i
     p.Y = Y_dev;
     p.ldx = ldx;
     p.ldy = ldy;
+    const int64_t x_bytes = b_bytes_of(x_rows, ldx, h->n_cols);
+    p.x_bytes = x_bytes <= kNearBytes ? (uint32_t)x_bytes : 0;
+    p.ldx_bytes = (uint32_t)(2 * ldx);
     p.n_rows = n_rows;
     p.k_tiles = h->k_tiles();
     p.tile_rows = h->tile_rows();
     p.steps = h->steps();
     p.half = (int32_t)h->rows();
     p.k_chunks = (int32_t)(h->n_cols / 32);
-    p.tiles_a_step = h->group < 128 ? 1 : h->group / 128;
+    const uint32_t tiles_a_step = h->group <= 128 ? 1 : (uint32_t)h->group / 128;
+    p.step_divide = tiles_a_step == 1 ? 0 : (uint32_t)(((1ull << 32) + tiles_a_step - 1) / tiles_a_step);      // (tiles and tiles_a_step are below 2^16)
     p.gated = h->gated;
     return p;
 }
@@ -815,13 +871,16 @@ void set_y(MmParams &p, int32_t y_type)
     p.fours = p.ldy % 4 == 0 && aligned(p.Y, p.f32 ? 16 : 8);
 }
 
-int launch_mm(const q4 *h, MmParams &p, int32_t rows, int64_t row_tiles, void *hip_stream)
+int launch_mm(const q4 *h, MmParams &p, int32_t rows, int64_t row_tiles, int64_t rows_each, void *hip_stream)
 {
-    const char *e1 = getenv("Q4_SPLIT"), *e2 = getenv("Q4_WAVES");
-    const int split = e1 ? atoi(e1) : rows == 16 ? 2 : row_tiles * ((p.tile_rows + 15) / 16) < 512 ? 2 : 0;
-    const int waves = e2 ? atoi(e2) : rows == 16 ? 4 : 8;
-    const Variant v = h->dtype == VBR_F16 ? mm_variant<VBR_F16>(h->group, h->zeros, rows, split, waves) : mm_variant<VBR_BF16>(h->group, h->zeros, rows, split, waves);
+    if (rows == 16 && p.x_bytes == 0) rows = 32;       // an X of 4 GiB and more: the other kernels have 64-bit addresses
+    Choice c = choose(p, rows, row_tiles, rows_each);
+    if (const char *e = getenv("Q4_NT")) c.nt = atoi(e);
+    if (const char *e = getenv("Q4_WAVES")) c.waves = atoi(e);
+    const Variant v = h->dtype == VBR_F16 ? mm_variant<VBR_F16>(h->group, h->zeros, c) : mm_variant<VBR_BF16>(h->group, h->zeros, c);
     p.col_blocks = (int32_t)((p.tile_rows + v.tile_rows - 1) / v.tile_rows);
+    p.by_col_blocks = Divide::by(p.col_blocks);
+    p.lg_waves = __builtin_ctz(v.threads / 64);
     const int64_t grid = row_tiles * p.col_blocks;
     if (grid > INT32_MAX) return VBR_EUNSUPPORTED;
     hipLaunchKernelGGL(v.kernel, dim3((unsigned)grid), dim3(v.threads), v.lds, static_cast<hipStream_t>(hip_stream), p);
@@ -900,10 +959,10 @@ extern "C" int q4_mm(const q4_t *h, const void *X_dev, int64_t ldx, void *Y_dev,
     if (rc != VBR_OK) return rc;
     if (h->n_mats != 1) return VBR_EINVAL;
     if (n_rows == 0) return VBR_OK;
-    MmParams p = mm_params(h, X_dev, ldx, Y_dev, ldy, n_rows);
+    MmParams p = mm_params(h, X_dev, ldx, n_rows, Y_dev, ldy, n_rows);
     set_y(p, y_type);
     const int32_t rows = n_rows <= 16 ? 16 : n_rows <= 32 ? 32 : 64;
-    return launch_mm(h, p, rows, (n_rows + rows - 1) / rows, hip_stream);
+    return launch_mm(h, p, rows, (n_rows + rows - 1) / rows, n_rows, hip_stream);
 }
 
 extern "C" int q4_mm_routed(const q4_t *h, const void *plan_dev, int64_t n_pairs, const void *X_dev, int64_t ldx, int64_t n_rows, void *Y_dev, int64_t ldy, int32_t y_type, void *hip_stream)
@@ -913,18 +972,14 @@ extern "C" int q4_mm_routed(const q4_t *h, const void *plan_dev, int64_t n_pairs
     if (!plan_sizes_ok(n_pairs, (int32_t)h->n_mats)) return VBR_EUNSUPPORTED;
     if (n_pairs == 0) return VBR_OK;
     if (!plan_dev || !aligned(plan_dev, 256) || n_rows < 1 || n_pairs % n_rows != 0) return VBR_EINVAL;
-    MmParams p = mm_params(h, X_dev, ldx, Y_dev, ldy, n_pairs);
+    MmParams p = mm_params(h, X_dev, ldx, n_rows, Y_dev, ldy, n_pairs);
     const PlanParts parts = plan_parts(n_pairs, (int32_t)h->n_mats);
     const char *d = static_cast<const char *>(plan_dev);
     p.order = reinterpret_cast<const int32_t *>(d + parts.order);
     p.plan_tiles = reinterpret_cast<const PlanTile *>(d + parts.tiles);
-    // i / d for i below 2^31: 2^(31 + l) / d rounded up, l the bits of d - 1
-    const int64_t d_rows = n_pairs / n_rows;
-    const int l = d_rows > 1 ? 64 - __builtin_clzll((unsigned long long)d_rows - 1) : 0;
-    p.divide = (uint32_t)(((1ull << (31 + l)) + d_rows - 1) / d_rows);
-    p.divide_shift = 31 + l;
+    p.by_places = Divide::by(n_pairs / n_rows);
     set_y(p, y_type);
-    return launch_mm(h, p, parts.tile_rows, parts.n_tiles, hip_stream);
+    return launch_mm(h, p, parts.tile_rows, parts.n_tiles, n_pairs / h->n_mats, hip_stream);
 }
 
 extern "C" void q4_free(q4_t *h) { delete h; }
