@@ -14,6 +14,7 @@ namespace vbrk {
 namespace {
 
 constexpr int kRouteThreads = 256;     // 4 waves
+constexpr int64_t kNarrowRows = 4096;  // rows from which on 16 lanes have one
 
 template <int TY>
 __device__ __forceinline__ float load_as_f32(const void *p, int64_t i)
@@ -31,35 +32,87 @@ __device__ __forceinline__ void store_f32(void *p, int64_t i, float v)          
     else static_cast<__bf16 *>(p)[i] = (__bf16)v;
 }
 
-template <class T>
-__device__ __forceinline__ T wave_max(T v)
+// exp(x), x at most a little above 0, within three steps: 2^t (1 + r), r what rounding took from t = x log2(e); 0 for -inf
+__device__ __forceinline__ float exp_of(float x)
 {
-    for (int m = 32; m; m >>= 1) {
-        const T o = __shfl_xor(v, m);
-        v = o > v ? o : v;
+    constexpr float log2e = 1.44269502f, rest = 1.92596299e-8f, ln2 = 0.693147181f;      // log2(e) in two numbers
+    x = fmaxf(x, -200.f);
+    const float t = x * log2e, r = __builtin_fmaf(x, rest, __builtin_fmaf(x, log2e, -t)), e = __builtin_amdgcn_exp2f(t);
+    return __builtin_fmaf(e, r * ln2, e);
+}
+__device__ __forceinline__ float sigmoid_of(float x)
+{
+    const float e = exp_of(-fabsf(x)), d = __builtin_amdgcn_rcpf(1.f + e);
+    return x < 0.f ? e * d : d;
+}
+
+// LP lanes have a row: all of them get the result.  16 lanes are one row of the vector unit.
+template <int CTRL>
+__device__ __forceinline__ uint32_t from_lane(uint32_t x) { return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, CTRL, 0xf, 0xf, true); }
+
+template <int LP, class Op>
+__device__ __forceinline__ uint32_t over_lanes(uint32_t x, Op op)
+{
+    x = op(x, from_lane<0xB1>(x));
+    x = op(x, from_lane<0x4E>(x));
+    x = op(x, from_lane<0x141>(x));
+    x = op(x, from_lane<0x140>(x));
+    if constexpr (LP == 64) {
+        const auto a = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+        x = op((uint32_t)a[0], (uint32_t)a[1]);
+        const auto b = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+        x = op((uint32_t)b[0], (uint32_t)b[1]);
     }
-    return v;
+    return x;
+}
+__device__ __forceinline__ uint32_t bits(float x) { return __builtin_bit_cast(uint32_t, x); }
+__device__ __forceinline__ float number(uint32_t x) { return __builtin_bit_cast(float, x); }
+template <int LP>
+__device__ __forceinline__ float row_max(float x) { return number(over_lanes<LP>(bits(x), [](uint32_t a, uint32_t b) { return bits(fmaxf(number(a), number(b))); })); }
+template <int LP>
+__device__ __forceinline__ float row_sum(float x) { return number(over_lanes<LP>(bits(x), [](uint32_t a, uint32_t b) { return bits(number(a) + number(b)); })); }
+template <int LP>
+__device__ __forceinline__ int row_min(int x) { return (int)over_lanes<LP>((uint32_t)x, [](uint32_t a, uint32_t b) { return a < b ? a : b; }); }     // none is negative
+template <int LP>
+__device__ __forceinline__ double row_max(double x)
+{
+    for (int m = LP / 2; m; m >>= 1) x = fmax(x, __shfl_xor(x, m));
+    return x;
+}
+template <int LP>
+__device__ __forceinline__ double row_sum(double x)
+{
+    for (int m = LP / 2; m; m >>= 1) x += __shfl_xor(x, m);
+    return x;
 }
 
-template <class T>
-__device__ __forceinline__ T wave_sum(T v)
+// V consecutive experts of a row, the first of them e0; those that are not there are closed
+template <int TY, int V>
+__device__ __forceinline__ void load_row(const void *p, int64_t row, int e0, int n_experts, bool whole, float (&l)[V])
 {
-    for (int m = 32; m; m >>= 1) v += __shfl_xor(v, m);
-    return v;
-}
-
-// (key, index) of the largest key, of equal ones the lowest index, in every lane
-__device__ __forceinline__ void wave_best(double &key, int &index)
-{
-    for (int m = 32; m; m >>= 1) {
-        const double k = __shfl_xor(key, m);
-        const int i = __shfl_xor(index, m);
-        if (k > key || (k == key && i < index)) {
-            key = k;
-            index = i;
+    constexpr int kBytes = V * (TY == VBR_F32 ? 4 : 2);
+    if constexpr (kBytes >= 16) {
+        if (whole) {
+#pragma unroll
+            for (int c = 0; c < kBytes / 16; ++c) {
+                const uint4v w = reinterpret_cast<const uint4v *>(static_cast<const char *>(p) + (row + e0) * (TY == VBR_F32 ? 4 : 2))[c];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t x = w[j];
+                    if constexpr (TY == VBR_F32) l[4 * c + j] = number(x);
+                    else if constexpr (TY == VBR_BF16) { l[8 * c + 2 * j] = number(x << 16); l[8 * c + 2 * j + 1] = number(x & 0xFFFF0000u); }
+                    else { l[8 * c + 2 * j] = (float)__builtin_bit_cast(_Float16, (uint16_t)x); l[8 * c + 2 * j + 1] = (float)__builtin_bit_cast(_Float16, (uint16_t)(x >> 16)); }
+                }
+            }
+            return;
         }
     }
+#pragma unroll
+    for (int v = 0; v < V; ++v) l[v] = e0 + v < n_experts ? load_as_f32<TY>(p, row + e0 + v) : -INFINITY;
 }
+
+// A raw score as it counts: NaN closes the expert like -inf, +inf is the largest finite number.
+__device__ __forceinline__ float raw_score(float l) { return l > -INFINITY ? fminf(l, FLT_MAX) : -INFINITY; }
 
 struct TopkParams {
     const void *logits;
@@ -68,134 +121,164 @@ struct TopkParams {
     float *weights;
     int64_t ld, n_rows;
     int32_t n_experts, top_k, n_groups, top_groups, group_size;
+    uint32_t group_factor;                     // expert e is of group e group_factor >> 20
     int32_t sigmoid, renormalise, scored;      // scored: the keys are scores with their biases, not the raw scores
+    int32_t whole, whole_bias;                 // rows are whole numbers of 16-byte pieces for each lane; the biases are
     float scale;
 };
 
-// A raw score as it counts: NaN closes the expert like -inf, +inf is the largest finite number.
-__device__ __forceinline__ float raw_score(float l) { return l > -INFINITY ? fminf(l, FLT_MAX) : -INFINITY; }
+// The choice among the keys, V a lane: lane j of the row gets the j-th expert, -1 without one.  Of equal keys the lower index wins.  Keys of type float may be
+// off by half of `bound`: then the result says whether any difference that decides is no larger than that.
+template <int LP, int V, class Key>
+__device__ __forceinline__ bool choose(const TopkParams &p, Key (&key)[V], float (&l)[V], Key *lds, int sub, int &my_id, Key bound)
+{
+    constexpr bool kCheck = sizeof(Key) == 4;
+    bool unsure = false;
+    if (p.n_groups > p.top_groups) {
+        // keys by way of LDS (one more place after every 16, or lanes meet in the same bank), a group a lane
+#pragma unroll
+        for (int v = 0; v < V; ++v) lds[(sub * V + v) + ((sub * V + v) >> 4)] = key[v];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        Key best = -INFINITY, second = -INFINITY;
+        if (sub < p.n_groups) {
+#pragma unroll 4
+            for (int i = 0; i < p.group_size; ++i) {
+                const int e = sub * p.group_size + i;
+                const Key x = lds[e + (e >> 4)];
+                second = x > best ? best : x > second ? x : second;
+                best = x > best ? x : best;
+            }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        Key mine = second > -INFINITY ? best + second : best, before = INFINITY;
+        uint64_t chosen = 0;
+        for (int i = 0; i < p.top_groups + (kCheck ? 1 : 0); ++i) {
+            const Key top = row_max<LP>(mine);
+            const int at = row_min<LP>(mine == top && top > -INFINITY ? sub : INT_MAX);
+            if (i == p.top_groups) unsure = top > -INFINITY && before - top <= 2 * bound;      // (a sum of two keys is off by twice as much)
+            else if (at != INT_MAX) chosen |= 1ull << at;
+            if (sub == at) mine = -INFINITY;
+            before = top;
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            if (sub * V + v < p.n_experts && !(chosen >> ((uint32_t)(sub * V + v) * p.group_factor >> 20) & 1)) key[v] = -INFINITY;
+    }
+    const bool by_raw = p.bias == nullptr;                // the same order, and exact
+    if (by_raw && p.scored) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) key[v] = key[v] > -INFINITY ? (Key)l[v] : (Key)-INFINITY;
+    }
+    Key before = INFINITY;
+    for (int j = 0; j < p.top_k + (kCheck && !by_raw ? 1 : 0); ++j) {
+        Key top = key[0];
+#pragma unroll
+        for (int v = 1; v < V; ++v) top = key[v] > top ? key[v] : top;
+        int mine = 0;
+#pragma unroll
+        for (int v = V - 1; v > 0; --v) mine = key[v] == top ? v : mine;
+        if (key[0] == top) mine = 0;
+        const Key most = row_max<LP>(top);
+        const int at = row_min<LP>(top == most && most > -INFINITY ? sub * V + mine : INT_MAX);
+        if (kCheck && !by_raw) unsure |= most > -INFINITY && before - most <= bound;
+        before = most;
+        if (j < p.top_k && sub == j) my_id = at == INT_MAX ? -1 : at;
+        const int taken = at - sub * V;
+#pragma unroll
+        for (int v = 0; v < V; ++v) key[v] = taken == v ? (Key)-INFINITY : key[v];
+    }
+    return unsure;
+}
 
-// One wave a row, V experts a lane.  Sums of scores and biases are compared in 64 bits: two of them that 32 bits cannot tell apart would let
-// their order depend on how they were rounded.  Raw scores are compared as they are, since the score rises with them.
-template <int TY, int V>
+// LP lanes a row, V experts a lane.  What decides between sums of scores and biases are differences that 32 bits may not tell: they are made in 32 bits, with a
+// bound for what they are off by, and where a difference is within it, in 64 bits.  Raw scores are compared as they are: the score rises with them.
+template <int TY, int LP, int V>
 __global__ void __launch_bounds__(kRouteThreads) route_topk_kernel(const TopkParams p)
 {
-    __shared__ double keys[kRouteThreads / 64][64 * V];
-    const int lane = threadIdx.x & 63, in_wg = threadIdx.x >> 6;
-    const int64_t row = (int64_t)blockIdx.x * (kRouteThreads / 64) + in_wg;
-    if (row >= p.n_rows) return;
-    float l[V];
-    double key[V];
+    constexpr int kRows = kRouteThreads / LP;
+    __shared__ double keys[kRows][LP * V + LP * V / 16];
+    const int sub = threadIdx.x % LP, in_wg = threadIdx.x / LP;
+    const int64_t wanted = (int64_t)blockIdx.x * kRows + in_wg, row = wanted < p.n_rows ? wanted : p.n_rows - 1;
+    float l[V], key[V];
+    load_row<TY, V>(p.logits, row * p.ld, sub * V, p.n_experts, p.whole && (sub + 1) * V <= p.n_experts, l);
+    float top = -INFINITY, total = 1.f;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        const int e = lane * V + v;
-        l[v] = e < p.n_experts ? raw_score(load_as_f32<TY>(p.logits, row * p.ld + e)) : -INFINITY;
+        l[v] = raw_score(l[v]);
+        top = fmaxf(top, l[v]);
     }
-    float top = -INFINITY;
+    const bool softmax_sum = !p.sigmoid && (p.scored || !p.renormalise);
+    if (softmax_sum) {
+        top = row_max<LP>(top);
+        total = 0.f;
 #pragma unroll
-    for (int v = 0; v < V; ++v) top = fmaxf(top, l[v]);
-    top = wave_max(top);
-    double total = 0;
-    if (!p.sigmoid && top > -INFINITY) {
-#pragma unroll
-        for (int v = 0; v < V; ++v) total += l[v] > -INFINITY ? exp((double)l[v] - (double)top) : 0.0;
-        total = wave_sum(total);
+        for (int v = 0; v < V; ++v) total += l[v] > -INFINITY ? exp_of(l[v] - top) : 0.f;
+        total = row_sum<LP>(total);
     }
-    auto score = [&](float x) { return p.sigmoid ? 1.0 / (1.0 + exp(-(double)x)) : exp((double)x - (double)top) / total; };
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-        key[v] = -INFINITY;
-        if (l[v] > -INFINITY) {
-            if (p.scored) {
-                key[v] = score(l[v]) + (p.bias ? (double)p.bias[lane * V + v] : 0.0);
-                if (!(key[v] > -INFINITY)) key[v] = -INFINITY;
-            } else {
-                key[v] = (double)l[v];
-            }
-        }
-    }
-    if (p.n_groups > 1) {
-#pragma unroll
-        for (int v = 0; v < V; ++v) keys[in_wg][lane * V + v] = key[v];
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        double best = -INFINITY, second = -INFINITY;
-        if (lane < p.n_groups) {
-            for (int i = 0; i < p.group_size; ++i) {
-                const double x = keys[in_wg][lane * p.group_size + i];
-                if (x > best) {
-                    second = best;
-                    best = x;
-                } else if (x > second) {
-                    second = x;
-                }
-            }
-        }
-        double mine = second > -INFINITY ? best + second : best;
-        uint64_t chosen = 0;
-        for (int i = 0; i < p.top_groups; ++i) {
-            double k = mine;
-            int at = mine > -INFINITY ? lane : INT_MAX;
-            wave_best(k, at);
-            if (at == INT_MAX) break;
-            chosen |= 1ull << at;
-            if (lane == at) mine = -INFINITY;
-        }
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const int e = lane * V + v;
-            if (e < p.n_experts && !(chosen >> (e / p.group_size) & 1)) key[v] = -INFINITY;
-        }
-    }
-    // lane j keeps the j-th choice
     int my_id = -1;
-    float my_raw = -INFINITY;
-    if (!p.scored || p.bias == nullptr) {
+    bool unsure;
+    if (p.scored) {
+        float bias[V];
+        if (p.bias) {
+            load_row<VBR_F32, V>(p.bias, 0, sub * V, p.n_experts, p.whole_bias && (sub + 1) * V <= p.n_experts, bias);
+        } else {
 #pragma unroll
-        for (int v = 0; v < V; ++v) key[v] = key[v] > -INFINITY ? (double)l[v] : -INFINITY;
+            for (int v = 0; v < V; ++v) bias[v] = 0.f;
+        }
+        float widest = 0.f;
+        const float one_of_total = 1.f / total;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const float s = (p.sigmoid ? sigmoid_of(l[v]) : exp_of(l[v] - top) * one_of_total) + bias[v];
+            key[v] = l[v] > -INFINITY && s > -INFINITY ? s : -INFINITY;
+            widest = fmaxf(widest, fabsf(key[v]) < INFINITY ? fabsf(key[v]) : 0.f);
+        }
+        widest = row_max<LP>(widest);
+        // A sigmoid is off by 8 half steps of 1 at most (exponential, sum, reciprocal, product), a softmax by those and what V + 6 additions in a row
+        // leave in its sum, and the sum with the bias by half a step of itself; two of them differ by as much again.
+        unsure = choose<LP, V>(p, key, l, reinterpret_cast<float *>(keys[in_wg]), sub, my_id, 0x1p-24f * (2 * (p.sigmoid ? 8 : 18 + V) + 4 * widest));
+    } else {
+#pragma unroll
+        for (int v = 0; v < V; ++v) key[v] = l[v];
+        unsure = choose<LP, V>(p, key, l, reinterpret_cast<float *>(keys[in_wg]), sub, my_id, 0.f);
     }
-    for (int j = 0; j < p.top_k; ++j) {
-        double k = -INFINITY;
-        int at = INT_MAX;
-        float raw = 0;
+    if (__builtin_expect(__ballot(unsure) != 0, 0)) {
+        double all = 0;
+        if (!p.sigmoid) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) all += l[v] > -INFINITY ? exp((double)l[v] - (double)top) : 0.0;
+            all = row_sum<LP>(all);
+        }
+        double exact[V];
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            if (key[v] > k) {
-                k = key[v];
-                at = lane * V + v;
+            exact[v] = -INFINITY;
+            if (l[v] > -INFINITY) {
+                const double s = p.sigmoid ? 1.0 / (1.0 + exp(-(double)l[v])) : exp((double)l[v] - (double)top) / all;
+                exact[v] = s + (p.bias ? (double)p.bias[sub * V + v] : 0.0);
+                if (!(exact[v] > -INFINITY)) exact[v] = -INFINITY;
             }
         }
-        wave_best(k, at);
-        if (at == INT_MAX) break;
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            if (at == lane * V + v) {
-                raw = l[v];
-                key[v] = -INFINITY;
-            }
-        }
-        raw = __shfl(raw, at / V);
-        if (lane == j) {
-            my_id = at;
-            my_raw = raw;
-        }
+        my_id = -1;
+        choose<LP, V>(p, exact, l, keys[in_wg], sub, my_id, 0.0);
     }
     // Renormalised, the scores are taken relative to the largest chosen one, so that no sum is zero however low they are.
-    double w = 0;
+    const float raw = my_id >= 0 ? raw_score(load_as_f32<TY>(p.logits, row * p.ld + my_id)) : -INFINITY;
+    float w = 0.f;
     if (p.renormalise) {
-        const float x = p.sigmoid ? fminf(my_raw, 0.f) : my_raw;
-        const float most = wave_max(my_id >= 0 ? x : -INFINITY);
+        const float x = p.sigmoid ? fminf(raw, 0.f) : raw, most = row_max<LP>(x);
         if (my_id >= 0) {
-            w = exp((double)x - (double)most);
-            if (p.sigmoid) w /= 1.0 + exp(-fabs((double)my_raw));
+            w = exp_of(x - most);
+            if (p.sigmoid) w /= 1.f + exp_of(-fabsf(raw));
         }
-        const double sum = wave_sum(w);
+        const float sum = row_sum<LP>(w);
         if (my_id >= 0) w /= sum;
     } else if (my_id >= 0) {
-        w = score(my_raw);
+        w = p.sigmoid ? sigmoid_of(raw) : exp_of(raw - top) / total;
     }
-    if (lane < p.top_k) {
-        p.ids[row * p.top_k + lane] = my_id;
-        p.weights[row * p.top_k + lane] = (float)(w * p.scale);
+    if (sub < p.top_k && wanted < p.n_rows) {
+        p.ids[row * p.top_k + sub] = my_id;
+        p.weights[row * p.top_k + sub] = w * p.scale;
     }
 }
 
@@ -206,6 +289,7 @@ struct TopkGradParams {
     void *dlogits;
     int64_t ld, ldd, n_rows;
     int32_t n_experts, top_k, sigmoid, renormalise;
+    int32_t whole, whole_out;
     float scale;
 };
 
@@ -213,65 +297,84 @@ struct TopkGradParams {
 //   renormalised   dl = scale r_j (dw_j - c), times (1 - s_j) for sigmoids, at the chosen experts, zero elsewhere
 //   sigmoid        dl = scale dw_j s_j (1 - s_j) at the chosen ones
 //   softmax        dl = scale p_e (dw_e - sum_j dw_j p_j) everywhere
-template <int TY, int V>
+// Only the last one reads all raw scores.
+template <int TY, int LP, int V>
 __global__ void __launch_bounds__(kRouteThreads) route_topk_grad_kernel(const TopkGradParams p)
 {
-    const int lane = threadIdx.x & 63, in_wg = threadIdx.x >> 6;
-    const int64_t row = (int64_t)blockIdx.x * (kRouteThreads / 64) + in_wg;
-    if (row >= p.n_rows) return;
-    int id = lane < p.top_k ? p.ids[row * p.top_k + lane] : -1;
+    constexpr int kRows = kRouteThreads / LP;
+    const int sub = threadIdx.x % LP;
+    const int64_t wanted = (int64_t)blockIdx.x * kRows + threadIdx.x / LP, row = wanted < p.n_rows ? wanted : p.n_rows - 1;
+    int id = sub < p.top_k ? p.ids[row * p.top_k + sub] : -1;
     if (id >= p.n_experts) id = -1;
     const float raw = id >= 0 ? raw_score(load_as_f32<TY>(p.logits, row * p.ld + id)) : -INFINITY;
-    const bool there = raw > -INFINITY;
-    const float dw = there ? p.dweights[row * p.top_k + lane] : 0.f;
-    const bool everywhere = !p.sigmoid && !p.renormalise;
-    float l[V];
-    float top = -INFINITY, total = 0.f;
+    const bool there = raw > -INFINITY, everywhere = !p.sigmoid && !p.renormalise;
+    const float dw = there ? p.dweights[row * p.top_k + sub] : 0.f;
+    float l[V], top = -INFINITY, total = 0.f;
     if (everywhere) {
+        load_row<TY, V>(p.logits, row * p.ld, sub * V, p.n_experts, p.whole && (sub + 1) * V <= p.n_experts, l);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const int e = lane * V + v;
-            l[v] = e < p.n_experts ? raw_score(load_as_f32<TY>(p.logits, row * p.ld + e)) : -INFINITY;
+            l[v] = raw_score(l[v]);
             top = fmaxf(top, l[v]);
         }
-        top = wave_max(top);
+        top = row_max<LP>(top);
 #pragma unroll
-        for (int v = 0; v < V; ++v) total += l[v] > -INFINITY ? expf(l[v] - top) : 0.f;
-        total = wave_sum(total);
+        for (int v = 0; v < V; ++v) {
+            l[v] = l[v] > -INFINITY ? exp_of(l[v] - top) : 0.f;
+            total += l[v];
+        }
+        total = row_sum<LP>(total);
     }
-    float s = 0.f, mine = 0.f, common = 0.f;        // this place's part of the gradient, and what every expert's has of the sum
+    float mine = 0.f, common = 0.f;                 // this place's part of the gradient, and what every expert's has of the sum
     if (p.renormalise) {
-        const float x = p.sigmoid ? fminf(raw, 0.f) : raw;
-        const float most = wave_max(there ? x : -INFINITY);
-        if (there) s = expf(x - most);
-        float rest = 1.f;
+        const float x = p.sigmoid ? fminf(raw, 0.f) : raw, most = row_max<LP>(x);
+        float s = there ? exp_of(x - most) : 0.f, rest = 1.f;
         if (there && p.sigmoid) {
-            const float e = expf(-fabsf(raw));
+            const float e = exp_of(-fabsf(raw));
             s /= 1.f + e;
             rest = (raw > 0.f ? e : 1.f) / (1.f + e);           // 1 - sigmoid(raw)
         }
-        const float sum = wave_sum(s), r = there ? s / sum : 0.f;
-        mine = p.scale * r * (dw - wave_sum(dw * r)) * rest;
+        const float sum = row_sum<LP>(s), r = there ? s / sum : 0.f;
+        mine = p.scale * r * (dw - row_sum<LP>(dw * r)) * rest;
     } else if (p.sigmoid) {
-        const float e = expf(-fabsf(raw));
+        const float e = exp_of(-fabsf(raw));
         mine = there ? p.scale * dw * e / ((1.f + e) * (1.f + e)) : 0.f;
     } else {
-        s = there ? expf(raw - top) / total : 0.f;
-        mine = p.scale * s * dw;
-        common = wave_sum(mine);
+        mine = there ? p.scale * dw * (exp_of(raw - top) / total) : 0.f;
+        common = row_sum<LP>(mine);
     }
     float out[V];
 #pragma unroll
-    for (int v = 0; v < V; ++v) out[v] = everywhere && l[v] > -INFINITY ? -common * (expf(l[v] - top) / total) : 0.f;
+    for (int v = 0; v < V; ++v) out[v] = everywhere && total > 0.f ? -common * (l[v] / total) : 0.f;
     for (int j = 0; j < p.top_k; ++j) {
-        const int at = __shfl(id, j);
-        const float g = __shfl(mine, j);
+        const int at = __shfl(id, j, LP) - sub * V;
+        const float g = __shfl(mine, j, LP);
 #pragma unroll
-        for (int v = 0; v < V; ++v) out[v] += at == lane * V + v ? g : 0.f;
+        for (int v = 0; v < V; ++v) out[v] += at == v ? g : 0.f;
+    }
+    if (wanted >= p.n_rows) return;
+    constexpr int kBytes = V * (TY == VBR_F32 ? 4 : 2);
+    if constexpr (kBytes >= 16) {
+        if (p.whole_out && (sub + 1) * V <= p.n_experts) {
+#pragma unroll
+            for (int c = 0; c < kBytes / 16; ++c) {
+                uint4v w;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if constexpr (TY == VBR_F32) w[j] = bits(out[4 * c + j]);
+                    else if constexpr (TY == VBR_BF16)
+                        w[j] = (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)out[8 * c + 2 * j]) | (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)out[8 * c + 2 * j + 1]) << 16;
+                    else
+                        w[j] = (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)out[8 * c + 2 * j]) | (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)out[8 * c + 2 * j + 1]) << 16;
+                }
+                reinterpret_cast<uint4v *>(static_cast<char *>(p.dlogits) + (row * p.ldd + sub * V) * (TY == VBR_F32 ? 4 : 2))[c] = w;
+            }
+            return;
+        }
     }
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        const int e = lane * V + v;
+        const int e = sub * V + v;
         if (e < p.n_experts) store_f32<TY>(p.dlogits, row * p.ldd + e, out[v]);
     }
 }
@@ -487,7 +590,7 @@ __global__ void __launch_bounds__(kRouteThreads) route_combine_grad_kernel(const
         for (int i = 0; i < 8; ++i) g[i] = there ? g[i] * w : 0.f;
         store8<TY>(p.dy, pair * p.lddy + col, g);
     }
-    dot = wave_sum(dot);
+    dot = row_sum<64>(dot);
     if (lane == 0) p.dweights[pair] = dot;
 }
 
@@ -514,21 +617,40 @@ bool float_type(int32_t t) { return t == VBR_F16 || t == VBR_BF16 || t == VBR_F3
 bool aligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 int64_t up(int64_t x, int64_t q) { return (x + q - 1) / q * q; }
 
-#define ROUTE_LAUNCH(KERNEL, TY, V) hipLaunchKernelGGL((KERNEL<TY, V>), dim3(grid), dim3(kRouteThreads), 0, stream, p)
-#define ROUTE_BY_WIDTH(KERNEL, TY)                        \
-    do {                                                  \
-        if (n_experts <= 64) ROUTE_LAUNCH(KERNEL, TY, 1);       \
-        else if (n_experts <= 128) ROUTE_LAUNCH(KERNEL, TY, 2); \
-        else if (n_experts <= 256) ROUTE_LAUNCH(KERNEL, TY, 4); \
-        else if (n_experts <= 512) ROUTE_LAUNCH(KERNEL, TY, 8); \
-        else ROUTE_LAUNCH(KERNEL, TY, 16);                \
+// Lanes of a row: 16 where they can hold the experts and there are rows for every SIMD, four a wave, 64 elsewhere: one row of them is done sooner.
+struct Width {
+    int32_t lanes, each;
+};
+Width route_width(int32_t n_experts, int32_t top_k, int32_t n_groups, int64_t n_rows)
+{
+    const int32_t lanes = n_rows >= kNarrowRows && n_experts <= 256 && top_k <= 16 && n_groups <= 16 ? 16 : 64;
+    int32_t each = 1;
+    while (lanes * each < n_experts) each *= 2;
+    return {lanes, each};
+}
+
+#define ROUTE_LAUNCH(KERNEL, TY, LP, V) hipLaunchKernelGGL((KERNEL<TY, LP, V>), dim3(grid), dim3(kRouteThreads), 0, stream, p)
+#define ROUTE_BY_EACH(KERNEL, TY, LP)                         \
+    do {                                                      \
+        if (width.each == 1) ROUTE_LAUNCH(KERNEL, TY, LP, 1);      \
+        else if (width.each == 2) ROUTE_LAUNCH(KERNEL, TY, LP, 2); \
+        else if (width.each == 4) ROUTE_LAUNCH(KERNEL, TY, LP, 4); \
+        else if (width.each == 8) ROUTE_LAUNCH(KERNEL, TY, LP, 8); \
+        else ROUTE_LAUNCH(KERNEL, TY, LP, 16);                \
     } while (0)
-#define ROUTE_BY_TYPE(KERNEL, type)                       \
-    do {                                                  \
+#define ROUTE_BY_WIDTH(KERNEL, TY)                            \
+    do {                                                      \
+        if (width.lanes == 16) ROUTE_BY_EACH(KERNEL, TY, 16);      \
+        else ROUTE_BY_EACH(KERNEL, TY, 64);                   \
+    } while (0)
+#define ROUTE_BY_TYPE(KERNEL, type)                           \
+    do {                                                      \
         if (type == VBR_F32) ROUTE_BY_WIDTH(KERNEL, VBR_F32);      \
         else if (type == VBR_F16) ROUTE_BY_WIDTH(KERNEL, VBR_F16); \
-        else ROUTE_BY_WIDTH(KERNEL, VBR_BF16);            \
+        else ROUTE_BY_WIDTH(KERNEL, VBR_BF16);                \
     } while (0)
+
+bool whole_pieces(const void *rows, int64_t ld, uintptr_t size) { return aligned(rows, 16) && ld * (int64_t)size % 16 == 0; }
 
 }  // namespace
 
@@ -584,12 +706,15 @@ extern "C" int route_topk(const vbr_route_t *how, const void *logits_dev, int64_
     p.n_groups = how->n_groups;
     p.top_groups = how->top_groups;
     p.group_size = how->n_experts / how->n_groups;
+    p.group_factor = (uint32_t)((1 << 20) + p.group_size - 1) / (uint32_t)p.group_size;
     p.sigmoid = how->score == VBR_SIGMOID;
     p.renormalise = how->renormalise != 0;
     p.scored = bias_dev != nullptr || how->n_groups > 1;
     p.scale = how->scale;
-    const int n_experts = how->n_experts;
-    const unsigned grid = (unsigned)((n_rows + kRouteThreads / 64 - 1) / (kRouteThreads / 64));
+    p.whole = whole_pieces(logits_dev, ld, logits_type == VBR_F32 ? 4 : 2);
+    p.whole_bias = aligned(bias_dev, 16);
+    const Width width = route_width(how->n_experts, how->top_k, how->n_groups, n_rows);
+    const unsigned grid = (unsigned)((n_rows + kRouteThreads / width.lanes - 1) / (kRouteThreads / width.lanes));
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     ROUTE_BY_TYPE(route_topk_kernel, logits_type);
     return launched();
@@ -616,8 +741,10 @@ extern "C" int route_topk_grad(const vbr_route_t *how, const void *logits_dev, i
     p.sigmoid = how->score == VBR_SIGMOID;
     p.renormalise = how->renormalise != 0;
     p.scale = how->scale;
-    const int n_experts = how->n_experts;
-    const unsigned grid = (unsigned)((n_rows + kRouteThreads / 64 - 1) / (kRouteThreads / 64));
+    p.whole = whole_pieces(logits_dev, ld, size);
+    p.whole_out = whole_pieces(dlogits_dev, ldd, size);
+    const Width width = route_width(how->n_experts, how->top_k, 1, n_rows);
+    const unsigned grid = (unsigned)((n_rows + kRouteThreads / width.lanes - 1) / (kRouteThreads / width.lanes));
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     ROUTE_BY_TYPE(route_topk_grad_kernel, logits_type);
     return launched();
