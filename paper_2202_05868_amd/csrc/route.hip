@@ -121,71 +121,184 @@ struct TopkParams {
     float *weights;
     int64_t ld, n_rows;
     int32_t n_experts, top_k, n_groups, top_groups, group_size;
+    int32_t lanes_a_group;                     // a power of two of whole lanes; 0: none
     uint32_t group_factor;                     // expert e is of group e group_factor >> 20
     int32_t sigmoid, renormalise, scored;      // scored: the keys are scores with their biases, not the raw scores
     int32_t whole, whole_bias;                 // rows are whole numbers of 16-byte pieces for each lane; the biases are
     float scale;
 };
 
-// The choice among the keys, V a lane: lane j of the row gets the j-th expert, -1 without one.  Of equal keys the lower index wins.  Keys of type float may be
-// off by half of `bound`: then the result says whether any difference that decides is no larger than that.
-template <int LP, int V, class Key>
-__device__ __forceinline__ bool choose(const TopkParams &p, Key (&key)[V], float (&l)[V], Key *lds, int sub, int &my_id, Key bound)
+// The choice among the keys, V a lane, in 64 bits: lane j of the row gets the j-th expert, -1 without one.  Of equal keys the lower index wins.
+template <int LP, int V>
+__device__ __forceinline__ int choose_exactly(const TopkParams &p, double (&key)[V], const float (&l)[V], double *lds, int sub)
 {
-    constexpr bool kCheck = sizeof(Key) == 4;
-    bool unsure = false;
     if (p.n_groups > p.top_groups) {
         // keys by way of LDS (one more place after every 16, or lanes meet in the same bank), a group a lane
 #pragma unroll
         for (int v = 0; v < V; ++v) lds[(sub * V + v) + ((sub * V + v) >> 4)] = key[v];
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        Key best = -INFINITY, second = -INFINITY;
+        double best = -INFINITY, second = -INFINITY;
         if (sub < p.n_groups) {
-#pragma unroll 4
             for (int i = 0; i < p.group_size; ++i) {
                 const int e = sub * p.group_size + i;
-                const Key x = lds[e + (e >> 4)];
+                const double x = lds[e + (e >> 4)];
                 second = x > best ? best : x > second ? x : second;
                 best = x > best ? x : best;
             }
         }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        Key mine = second > -INFINITY ? best + second : best, before = INFINITY;
+        double mine = second > -INFINITY ? best + second : best;
         uint64_t chosen = 0;
-        for (int i = 0; i < p.top_groups + (kCheck ? 1 : 0); ++i) {
-            const Key top = row_max<LP>(mine);
+        for (int i = 0; i < p.top_groups; ++i) {
+            const double top = row_max<LP>(mine);
             const int at = row_min<LP>(mine == top && top > -INFINITY ? sub : INT_MAX);
-            if (i == p.top_groups) unsure = top > -INFINITY && before - top <= 2 * bound;      // (a sum of two keys is off by twice as much)
-            else if (at != INT_MAX) chosen |= 1ull << at;
+            if (at != INT_MAX) chosen |= 1ull << at;
             if (sub == at) mine = -INFINITY;
-            before = top;
         }
 #pragma unroll
         for (int v = 0; v < V; ++v)
             if (sub * V + v < p.n_experts && !(chosen >> ((uint32_t)(sub * V + v) * p.group_factor >> 20) & 1)) key[v] = -INFINITY;
     }
-    const bool by_raw = p.bias == nullptr;                // the same order, and exact
-    if (by_raw && p.scored) {
+    if (p.bias == nullptr) {                              // the same order, and exact
 #pragma unroll
-        for (int v = 0; v < V; ++v) key[v] = key[v] > -INFINITY ? (Key)l[v] : (Key)-INFINITY;
+        for (int v = 0; v < V; ++v) key[v] = key[v] > -INFINITY ? (double)l[v] : (double)-INFINITY;
     }
-    Key before = INFINITY;
-    for (int j = 0; j < p.top_k + (kCheck && !by_raw ? 1 : 0); ++j) {
-        Key top = key[0];
+    int my_id = -1;
+    for (int j = 0; j < p.top_k; ++j) {
+        double top = key[0];
 #pragma unroll
         for (int v = 1; v < V; ++v) top = key[v] > top ? key[v] : top;
         int mine = 0;
 #pragma unroll
-        for (int v = V - 1; v > 0; --v) mine = key[v] == top ? v : mine;
-        if (key[0] == top) mine = 0;
-        const Key most = row_max<LP>(top);
+        for (int v = V - 1; v >= 0; --v) mine = key[v] == top ? v : mine;
+        const double most = row_max<LP>(top);
         const int at = row_min<LP>(top == most && most > -INFINITY ? sub * V + mine : INT_MAX);
-        if (kCheck && !by_raw) unsure |= most > -INFINITY && before - most <= bound;
-        before = most;
-        if (j < p.top_k && sub == j) my_id = at == INT_MAX ? -1 : at;
+        if (sub == j) my_id = at == INT_MAX ? -1 : at;
         const int taken = at - sub * V;
 #pragma unroll
-        for (int v = 0; v < V; ++v) key[v] = taken == v ? (Key)-INFINITY : key[v];
+        for (int v = 0; v < V; ++v) key[v] = taken == v ? -INFINITY : key[v];
+    }
+    return my_id;
+}
+
+// Numbers as integers of the same order
+__device__ __forceinline__ int ordered(float x)
+{
+    const int i = (int)bits(x + 0.f);                     // (-0 is 0)
+    return i ^ (i >> 31 & INT_MAX);
+}
+__device__ __forceinline__ float of_ordered(int i) { return number((uint32_t)(i ^ (i >> 31 & INT_MAX))); }
+
+template <int LP>
+__device__ __forceinline__ int row_max_int(int x) { return (int)over_lanes<LP>((uint32_t)x, [](uint32_t a, uint32_t b) { return (uint32_t)((int)a > (int)b ? (int)a : (int)b); }); }
+
+// falling, by merging odd and even places: comparators that are known beforehand
+template <int V>
+__device__ __forceinline__ void sort_falling(int (&x)[V])
+{
+#pragma unroll
+    for (int p = 1; p < V; p *= 2)
+#pragma unroll
+        for (int k = p; k >= 1; k /= 2)
+#pragma unroll
+            for (int j = k % p; j + k < V; j += 2 * k)
+#pragma unroll
+                for (int i = 0; i < k; ++i)
+                    if (i + j + k < V && (i + j) / (2 * p) == (i + j + k) / (2 * p)) {
+                        const int a = x[i + j], b = x[i + j + k];
+                        x[i + j] = a > b ? a : b;
+                        x[i + j + k] = a > b ? b : a;
+                    }
+}
+
+constexpr int kClosed = INT_MIN;
+
+// The same in 32 bits.  Keys are whole numbers in the order of the numbers, with an expert's place in its lane in the lowest bits, lower places first: a lane sorts
+// its keys once, and a choice is the largest of the lanes' first ones.  `bound` is what the difference of two keys may be off by, before the lowest bits
+// are lost; the result says whether any difference that decides may be of the other sign.  exact: neither is; then there is nothing to say.
+template <int LP, int V>
+__device__ __forceinline__ bool choose(const TopkParams &p, const float (&key)[V], const float (&l)[V], float *lds, int sub, int &my_id, float bound, bool exact)
+{
+    bool unsure = false;
+    uint64_t chosen = ~0ull;
+    int x[V];
+    auto pack = [&](const float (&from)[V]) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) x[v] = key[v] > -INFINITY ? (ordered(fminf(from[v], FLT_MAX)) & -V) | (V - 1 - v) : kClosed;
+    };
+    const bool by_raw = p.bias == nullptr;                // the same order, and exact
+    const bool by_lanes = p.lanes_a_group && !by_raw;
+    if (!by_raw) {
+        pack(key);
+        sort_falling(x);
+    }
+    if (p.n_groups > p.top_groups) {
+        float mine, before = INFINITY, wide = bound;
+        int group = sub;
+        if (by_lanes) {
+            int best = x[0], second = V > 1 ? x[V > 1] : kClosed;
+            auto merge = [&](int b, int s) {
+                second = max(min(best, b), max(second, s));
+                best = max(best, b);
+            };
+            if (p.lanes_a_group >= 2) merge((int)from_lane<0xB1>((uint32_t)best), (int)from_lane<0xB1>((uint32_t)second));
+            if (p.lanes_a_group >= 4) merge((int)from_lane<0x4E>((uint32_t)best), (int)from_lane<0x4E>((uint32_t)second));
+            if (p.lanes_a_group >= 8) merge((int)from_lane<0x141>((uint32_t)best), (int)from_lane<0x141>((uint32_t)second));
+            mine = best == kClosed ? -INFINITY : of_ordered(best) + (second == kClosed ? 0.f : of_ordered(second));
+            group = sub / p.lanes_a_group;
+        } else {
+            // by way of LDS (one more place after every 16, or lanes meet in the same bank), a group a lane
+#pragma unroll
+            for (int v = 0; v < V; ++v) lds[(sub * V + v) + ((sub * V + v) >> 4)] = key[v];
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            float best = -INFINITY, second = -INFINITY;
+            if (sub < p.n_groups) {
+#pragma unroll 4
+                for (int i = 0; i < p.group_size; ++i) {
+                    const int e = sub * p.group_size + i;
+                    const float y = lds[e + (e >> 4)];
+                    second = fmaxf(fminf(y, best), second);
+                    best = fmaxf(best, y);
+                }
+            }
+            mine = second > -INFINITY ? best + second : best;
+        }
+        chosen = 0;
+        for (int i = 0; i <= p.top_groups; ++i) {
+            const float top = row_max<LP>(mine);
+            const int at = row_min<LP>(mine == top && top > -INFINITY ? group : INT_MAX);
+            if (i == p.top_groups) unsure = top > -INFINITY && before - top <= 2 * wide + (fabsf(before) + fabsf(top)) * (V * 0x1p-22f);      // two keys each
+            else if (at != INT_MAX) chosen |= 1ull << at;
+            if (group == at) mine = -INFINITY;
+            before = top;
+        }
+    }
+    if (by_raw) {
+        pack(l);
+        if (p.n_groups > p.top_groups) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) x[v] = chosen >> ((uint32_t)(sub * V + v) * p.group_factor >> 20) & 1 ? x[v] : kClosed;
+        }
+        sort_falling(x);
+    } else if (p.n_groups > p.top_groups) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) x[v] = chosen >> ((uint32_t)(sub * V + V - 1 - (x[v] & (V - 1))) * p.group_factor >> 20) & 1 ? x[v] : kClosed;
+        if (!by_lanes) sort_falling(x);                   // (by lanes, a lane has all or none)
+    }
+    const float by = by_raw ? 0.f : bound;
+    float before = INFINITY;
+    for (int j = 0; j < p.top_k + (exact ? 0 : 1); ++j) {
+        const int first = x[0] & -V, most = row_max_int<LP>(first), mine = sub * V + V - 1 - (x[0] & (V - 1));      // (places count among equal keys only)
+        const int at = row_min<LP>(first == most && most != kClosed ? mine : INT_MAX);
+        if (!exact) {
+            const float now = of_ordered(most);
+            unsure |= most != kClosed && before - now <= by + (fabsf(before) + fabsf(now)) * (V * 0x1p-23f);
+            before = now;
+        }
+        if (j < p.top_k && sub == j) my_id = at == INT_MAX ? -1 : at;
+        const bool taken = at == mine;
+#pragma unroll
+        for (int v = 0; v + 1 < V; ++v) x[v] = taken ? x[v + 1] : x[v];
+        x[V - 1] = taken ? kClosed : x[V - 1];
     }
     return unsure;
 }
@@ -234,33 +347,41 @@ __global__ void __launch_bounds__(kRouteThreads) route_topk_kernel(const TopkPar
             widest = fmaxf(widest, fabsf(key[v]) < INFINITY ? fabsf(key[v]) : 0.f);
         }
         widest = row_max<LP>(widest);
-        // A sigmoid is off by 8 half steps of 1 at most (exponential, sum, reciprocal, product), a softmax by those and what V + 6 additions in a row
+        // A sigmoid is off by 8 half steps at 1 at most (exponential, sum, reciprocal, product), a softmax by those and what V + 6 additions in a row
         // leave in its sum, and the sum with the bias by half a step of itself; two of them differ by as much again.
-        unsure = choose<LP, V>(p, key, l, reinterpret_cast<float *>(keys[in_wg]), sub, my_id, 0x1p-24f * (2 * (p.sigmoid ? 8 : 18 + V) + 4 * widest));
+        unsure = choose<LP, V>(p, key, l, reinterpret_cast<float *>(keys[in_wg]), sub, my_id, 0x1p-24f * (2 * (p.sigmoid ? 8 : 18 + V) + 4 * widest), false);
     } else {
-#pragma unroll
-        for (int v = 0; v < V; ++v) key[v] = l[v];
-        unsure = choose<LP, V>(p, key, l, reinterpret_cast<float *>(keys[in_wg]), sub, my_id, 0.f);
+        // numbers of 16 bits leave the lowest bits of 32 free, and nothing is lost
+        unsure = choose<LP, V>(p, l, l, reinterpret_cast<float *>(keys[in_wg]), sub, my_id, 0.f, TY != VBR_F32);
     }
     if (__builtin_expect(__ballot(unsure) != 0, 0)) {
         double all = 0;
-        if (!p.sigmoid) {
+        if (!p.sigmoid && p.scored) {
 #pragma unroll
-            for (int v = 0; v < V; ++v) all += l[v] > -INFINITY ? exp((double)l[v] - (double)top) : 0.0;
+            for (int v = 0; v < V; ++v) all += exp((double)fmaxf(l[v], -FLT_MAX) - (double)fmaxf(top, -FLT_MAX)) * (l[v] > -INFINITY ? 1.0 : 0.0);
             all = row_sum<LP>(all);
         }
         double exact[V];
+        if (p.scored) {
+            // (without branches, so that the exponentials of several experts are on their way at once)
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            exact[v] = -INFINITY;
-            if (l[v] > -INFINITY) {
-                const double s = p.sigmoid ? 1.0 / (1.0 + exp(-(double)l[v])) : exp((double)l[v] - (double)top) / all;
-                exact[v] = s + (p.bias ? (double)p.bias[sub * V + v] : 0.0);
-                if (!(exact[v] > -INFINITY)) exact[v] = -INFINITY;
+            for (int v = 0; v < V; ++v) {
+                const double x = fmaxf(l[v], -FLT_MAX), e = exp(p.sigmoid ? -x : x - (double)fmaxf(top, -FLT_MAX));
+                exact[v] = p.sigmoid ? 1.0 / (1.0 + e) : e / all;
             }
+            double bias[V];
+#pragma unroll
+            for (int v = 0; v < V; ++v) bias[v] = p.bias && sub * V + v < p.n_experts ? (double)p.bias[sub * V + v] : 0.0;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                exact[v] += bias[v];
+                if (!(l[v] > -INFINITY) || !(exact[v] > -INFINITY)) exact[v] = -INFINITY;
+            }
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v) exact[v] = l[v];
         }
-        my_id = -1;
-        choose<LP, V>(p, exact, l, keys[in_wg], sub, my_id, 0.0);
+        my_id = choose_exactly<LP, V>(p, exact, l, keys[in_wg], sub);
     }
     // Renormalised, the scores are taken relative to the largest chosen one, so that no sum is zero however low they are.
     const float raw = my_id >= 0 ? raw_score(load_as_f32<TY>(p.logits, row * p.ld + my_id)) : -INFINITY;
@@ -714,6 +835,8 @@ extern "C" int route_topk(const vbr_route_t *how, const void *logits_dev, int64_
     p.whole = whole_pieces(logits_dev, ld, logits_type == VBR_F32 ? 4 : 2);
     p.whole_bias = aligned(bias_dev, 16);
     const Width width = route_width(how->n_experts, how->top_k, how->n_groups, n_rows);
+    const int32_t lanes_a_group = p.group_size / width.each;
+    p.lanes_a_group = p.group_size % width.each == 0 && lanes_a_group <= 8 && (lanes_a_group & (lanes_a_group - 1)) == 0 ? lanes_a_group : 0;
     const unsigned grid = (unsigned)((n_rows + kRouteThreads / width.lanes - 1) / (kRouteThreads / width.lanes));
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     ROUTE_BY_TYPE(route_topk_kernel, logits_type);
