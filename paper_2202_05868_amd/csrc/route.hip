@@ -2,6 +2,7 @@
 // of the chosen (row, place) pairs by expert, and the weighted sum of a row's results with its gradients.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cfloat>
 #include <climits>
 #include <cstdint>
@@ -218,7 +219,7 @@ constexpr int kClosed = INT_MIN;
 template <int LP, int V>
 __device__ __forceinline__ bool choose(const TopkParams &p, const float (&key)[V], const float (&l)[V], float *lds, int sub, int &my_id, float bound, bool exact)
 {
-    bool unsure = false;
+    bool unsure = false;              // (the same in every lane of the row)
     uint64_t chosen = ~0ull;
     int x[V];
     auto pack = [&](const float (&from)[V]) {
@@ -291,7 +292,7 @@ __device__ __forceinline__ bool choose(const TopkParams &p, const float (&key)[V
         const int at = row_min<LP>(first == most && most != kClosed ? mine : INT_MAX);
         if (!exact) {
             const float now = of_ordered(most);
-            unsure |= most != kClosed && before - now <= by + (fabsf(before) + fabsf(now)) * (V * 0x1p-23f);
+            unsure |= j > 0 && most != kClosed && before - now <= by + (fabsf(before) + fabsf(now)) * (V * 0x1p-23f);
             before = now;
         }
         if (j < p.top_k && sub == j) my_id = at == INT_MAX ? -1 : at;
@@ -303,14 +304,53 @@ __device__ __forceinline__ bool choose(const TopkParams &p, const float (&key)[V
     return unsure;
 }
 
+// The choice for one row in 64 bits, by a whole wave: lane j has the j-th expert.
+template <int TY, int V>
+__device__ __forceinline__ int choose_row_exactly(const TopkParams &p, int64_t row, int lane, double *lds)
+{
+    float l[V], bias[V], top = -INFINITY;
+    load_row<TY, V>(p.logits, row * p.ld, lane * V, p.n_experts, false, l);
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        l[v] = raw_score(l[v]);
+        top = fmaxf(top, l[v]);
+        bias[v] = p.bias && lane * V + v < p.n_experts ? p.bias[lane * V + v] : 0.f;
+    }
+    double key[V];
+    if (p.scored) {
+        const double most = fmaxf(row_max<64>(top), -FLT_MAX);
+        double total = 0;
+        // (without branches, so that the exponentials of several experts are on their way at once)
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const double x = fmaxf(l[v], -FLT_MAX);
+            key[v] = exp(p.sigmoid ? -x : x - most);
+            total += l[v] > -INFINITY ? key[v] : 0.0;
+        }
+        if (!p.sigmoid) total = row_sum<64>(total);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            key[v] = (p.sigmoid ? 1.0 / (1.0 + key[v]) : key[v] / total) + (double)bias[v];
+            if (!(l[v] > -INFINITY) || !(key[v] > -INFINITY)) key[v] = -INFINITY;
+        }
+    } else {
+#pragma unroll
+        for (int v = 0; v < V; ++v) key[v] = l[v];
+    }
+    return choose_exactly<64, V>(p, key, l, lds, lane);
+}
+
 // LP lanes a row, V experts a lane.  What decides between sums of scores and biases are differences that 32 bits may not tell: they are made in 32 bits, with a
 // bound for what they are off by, and where a difference is within it, in 64 bits.  Raw scores are compared as they are: the score rises with them.
 template <int TY, int LP, int V>
 __global__ void __launch_bounds__(kRouteThreads) route_topk_kernel(const TopkParams p)
 {
     constexpr int kRows = kRouteThreads / LP;
-    __shared__ double keys[kRows][LP * V + LP * V / 16];
+    constexpr int kEachOf64 = LP * V < 64 ? 1 : LP * V / 64, kRowLds = LP * V + LP * V / 16, kWaveLds = std::max(64 / LP * kRowLds * 4, 64 * kEachOf64 * 17 / 16 * 8);
+    __shared__ __attribute__((aligned(16))) char all_lds[kRouteThreads / 64][kWaveLds];
+    char *lds = all_lds[threadIdx.x >> 6];
     const int sub = threadIdx.x % LP, in_wg = threadIdx.x / LP;
+    float *row_lds = reinterpret_cast<float *>(lds) + in_wg % (64 / LP) * kRowLds;
     const int64_t wanted = (int64_t)blockIdx.x * kRows + in_wg, row = wanted < p.n_rows ? wanted : p.n_rows - 1;
     float l[V], key[V];
     load_row<TY, V>(p.logits, row * p.ld, sub * V, p.n_experts, p.whole && (sub + 1) * V <= p.n_experts, l);
@@ -349,39 +389,19 @@ __global__ void __launch_bounds__(kRouteThreads) route_topk_kernel(const TopkPar
         widest = row_max<LP>(widest);
         // A sigmoid is off by 8 half steps at 1 at most (exponential, sum, reciprocal, product), a softmax by those and what V + 6 additions in a row
         // leave in its sum, and the sum with the bias by half a step of itself; two of them differ by as much again.
-        unsure = choose<LP, V>(p, key, l, reinterpret_cast<float *>(keys[in_wg]), sub, my_id, 0x1p-24f * (2 * (p.sigmoid ? 8 : 18 + V) + 4 * widest), false);
+        unsure = choose<LP, V>(p, key, l, row_lds, sub, my_id, 0x1p-24f * (2 * (p.sigmoid ? 8 : 18 + V) + 4 * widest), false);
     } else {
         // numbers of 16 bits leave the lowest bits of 32 free, and nothing is lost
-        unsure = choose<LP, V>(p, l, l, reinterpret_cast<float *>(keys[in_wg]), sub, my_id, 0.f, TY != VBR_F32);
+        unsure = choose<LP, V>(p, l, l, row_lds, sub, my_id, 0.f, TY != VBR_F32);
     }
-    if (__builtin_expect(__ballot(unsure) != 0, 0)) {
-        double all = 0;
-        if (!p.sigmoid && p.scored) {
-#pragma unroll
-            for (int v = 0; v < V; ++v) all += exp((double)fmaxf(l[v], -FLT_MAX) - (double)fmaxf(top, -FLT_MAX)) * (l[v] > -INFINITY ? 1.0 : 0.0);
-            all = row_sum<LP>(all);
-        }
-        double exact[V];
-        if (p.scored) {
-            // (without branches, so that the exponentials of several experts are on their way at once)
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const double x = fmaxf(l[v], -FLT_MAX), e = exp(p.sigmoid ? -x : x - (double)fmaxf(top, -FLT_MAX));
-                exact[v] = p.sigmoid ? 1.0 / (1.0 + e) : e / all;
-            }
-            double bias[V];
-#pragma unroll
-            for (int v = 0; v < V; ++v) bias[v] = p.bias && sub * V + v < p.n_experts ? (double)p.bias[sub * V + v] : 0.0;
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                exact[v] += bias[v];
-                if (!(l[v] > -INFINITY) || !(exact[v] > -INFINITY)) exact[v] = -INFINITY;
-            }
-        } else {
-#pragma unroll
-            for (int v = 0; v < V; ++v) exact[v] = l[v];
-        }
-        my_id = choose_exactly<LP, V>(p, exact, l, keys[in_wg], sub);
+    // rows in doubt, one after the other, by the whole wave
+    for (uint64_t doubt = __ballot(unsure); doubt != 0;) {
+        const int lane = threadIdx.x & 63, of_row = __builtin_ctzll(doubt) / LP;
+        const int64_t at = (int64_t)blockIdx.x * kRows + (threadIdx.x >> 6) * (64 / LP) + of_row;
+        const int id = choose_row_exactly<TY, kEachOf64>(p, at < p.n_rows ? at : p.n_rows - 1, lane, reinterpret_cast<double *>(lds));
+        const int mine = __shfl(id, sub);
+        if (lane / LP == of_row) my_id = mine;
+        doubt &= LP == 64 ? 0 : ~(((1ull << (LP & 63)) - 1) << (of_row * LP));
     }
     // Renormalised, the scores are taken relative to the largest chosen one, so that no sum is zero however low they are.
     const float raw = my_id >= 0 ? raw_score(load_as_f32<TY>(p.logits, row * p.ld + my_id)) : -INFINITY;
