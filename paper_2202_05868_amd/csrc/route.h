@@ -10,16 +10,16 @@ namespace vbrk {
 constexpr int32_t kMaxExperts = 1024;              // one thread of a workgroup each, in the scan
 constexpr int32_t kMaxTopK = 64, kMaxGroups = 64;  // one lane each
 constexpr int64_t kMaxPairs = 1 << 30;             // positions are 32 bits
-constexpr int32_t kPlanChunk = 1024;               // pairs a wave counts
+constexpr int64_t kPlanPart = 4096;                // pairs of a workgroup, at least, where there are several
 
 // Byte offsets in a plan: int32 offsets [n_experts + 1] at 0, int32 order [n_pairs], PlanTile tiles [n_tiles],
-// int32 counts [n_chunks][n_experts].
+// int32 counts [n_parts][n_experts].
 struct PlanTile {
     int32_t expert, first, count, unused;          // positions first .. first + count - 1 of the order; count 0: no tile
 };
 struct PlanParts {
     int64_t order, tiles, counts, total;
-    int64_t n_tiles, n_chunks;
+    int64_t n_tiles, n_parts, per_wave;
     int32_t tile_rows;
 };
 PlanParts plan_parts(int64_t n_pairs, int32_t n_experts);

@@ -520,8 +520,11 @@ __global__ void __launch_bounds__(kRouteThreads) route_topk_grad_kernel(const To
     }
 }
 
-// ---- the grouping.  A wave owns a chunk of consecutive pairs and counts its experts; one workgroup turns the counts into every chunk's
-// first positions; the waves go over their chunks again and put each pair where it belongs.  Pairs of an expert stay in their order.
+// ---- the grouping.  A workgroup owns consecutive pairs and each of its 16 waves a part of them, which it counts by expert in LDS.  With the counts of the
+// workgroups and waves before it a wave knows where its first pair of every expert belongs, goes over its pairs again and puts them there: pairs of an
+// expert stay in their order.  One workgroup needs no other's counts; of several, a first launch leaves them in the plan.
+constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64;
+
 __device__ __forceinline__ uint64_t same_id(int id, int bits)      // lanes with this lane's id
 {
     uint64_t m = ~0ull;
@@ -541,97 +544,142 @@ __device__ __forceinline__ int expert_of(const int32_t *ids, int64_t at, int64_t
 
 struct PlanParams {
     const int32_t *ids;
-    int32_t *offsets, *order, *counts;             // counts [n_chunks][n_experts]
+    int32_t *offsets, *order, *counts;             // counts [n_parts][n_experts]
     PlanTile *tiles;
-    int64_t n_pairs;
-    int32_t n_experts, bits, n_chunks, tile_rows, n_tiles;
+    int64_t n_pairs, per_part, per_wave;           // pairs of a workgroup and of a wave, multiples of 64
+    int32_t n_experts, bits, n_parts, tile_rows, n_tiles;
+    int32_t lg_lanes;                              // 2^lg_lanes threads, at least as many as experts, have a part's counts
 };
 
-__global__ void __launch_bounds__(64) plan_count_kernel(const PlanParams p)
+__global__ void __launch_bounds__(kPlanThreads) plan_count_kernel(const PlanParams p)
 {
-    extern __shared__ int32_t hist[];
-    const int lane = threadIdx.x;
-    for (int e = lane; e <= p.n_experts; e += 64) hist[e] = 0;
+    extern __shared__ int32_t count[];
+    for (int e = threadIdx.x; e < p.n_experts; e += kPlanThreads) count[e] = 0;
     __syncthreads();
-    const int64_t first = (int64_t)blockIdx.x * kPlanChunk;
-    const int64_t end = first + kPlanChunk < p.n_pairs ? first + kPlanChunk : p.n_pairs;
-    for (int64_t at = first; at < end; at += 64) {
-        const int id = expert_of(p.ids, at + lane, end, p.n_experts);
-        const uint64_t same = same_id(id, p.bits);
-        if (__builtin_ctzll(same) == lane) hist[id] += __popcll(same);
-        __syncthreads();
+    const int64_t first = blockIdx.x * p.per_part, end = first + p.per_part < p.n_pairs ? first + p.per_part : p.n_pairs;
+    for (int64_t at = first + threadIdx.x; at < end; at += kPlanThreads) {
+        const int id = expert_of(p.ids, at, end, p.n_experts);
+        if (id < p.n_experts) atomicAdd(&count[id], 1);          // (whole numbers: in any order the same)
     }
-    for (int e = lane; e < p.n_experts; e += 64) p.counts[(int64_t)blockIdx.x * p.n_experts + e] = hist[e];
+    __syncthreads();
+    for (int e = threadIdx.x; e < p.n_experts; e += kPlanThreads) p.counts[(int64_t)blockIdx.x * p.n_experts + e] = count[e];
 }
 
-constexpr int kScanThreads = 1024;     // one a expert
-
-__device__ __forceinline__ int scan_1024(int x, int *sums, int &total)      // exclusive sum over the workgroup's threads
+// exclusive sums over the workgroup's threads of two numbers at once
+__device__ __forceinline__ int2 scan_plan(int2 x, int2 *sums, int2 &total)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int up = x;
+    int2 up = x;
     for (int d = 1; d < 64; d <<= 1) {
-        const int o = __shfl_up(up, d);
-        if (lane >= d) up += o;
-    }
-    __syncthreads();
-    if (lane == 63) sums[wave] = up;
-    __syncthreads();
-    int before = 0;
-    total = 0;
-    for (int w = 0; w < kScanThreads / 64; ++w) {
-        if (w < wave) before += sums[w];
-        total += sums[w];
-    }
-    return before + up - x;
-}
-
-__global__ void __launch_bounds__(kScanThreads) plan_scan_kernel(const PlanParams p)
-{
-    __shared__ int sums[kScanThreads / 64];
-    const int e = threadIdx.x;
-    int count = 0;
-    if (e < p.n_experts)
-        for (int c = 0; c < p.n_chunks; ++c) count += p.counts[(int64_t)c * p.n_experts + e];
-    int total, n_tiles;
-    const int start = scan_1024(count, sums, total);
-    if (e < p.n_experts) {
-        p.offsets[e] = start;
-        int at = start;
-        for (int c = 0; c < p.n_chunks; ++c) {
-            int32_t *mine = p.counts + (int64_t)c * p.n_experts + e;
-            const int here = *mine;
-            *mine = at;
-            at += here;
+        const int a = __shfl_up(up.x, d), b = __shfl_up(up.y, d);
+        if (lane >= d) {
+            up.x += a;
+            up.y += b;
         }
     }
-    if (e == 0) p.offsets[p.n_experts] = total;
-    const int tiles = (count + p.tile_rows - 1) / p.tile_rows, tile = scan_1024(tiles, sums, n_tiles);
-    for (int i = 0; i < tiles; ++i) {
-        const int left = count - i * p.tile_rows;
-        p.tiles[tile + i] = {e, start + i * p.tile_rows, left < p.tile_rows ? left : p.tile_rows, 0};
+    if (lane == 63) sums[wave] = up;
+    __syncthreads();
+    int2 before = make_int2(0, 0);
+    total = before;
+#pragma unroll
+    for (int w = 0; w < kPlanWaves; ++w) {
+        const int2 s = sums[w];
+        if (w < wave) {
+            before.x += s.x;
+            before.y += s.y;
+        }
+        total.x += s.x;
+        total.y += s.y;
     }
-    for (int i = n_tiles + e; i < p.n_tiles; i += kScanThreads) p.tiles[i] = {0, 0, 0, 0};
-    for (int64_t i = total + (int64_t)e; i < p.n_pairs; i += kScanThreads) p.order[i] = -1;
+    return make_int2(before.x + up.x - x.x, before.y + up.y - x.y);
 }
 
-__global__ void __launch_bounds__(64) plan_scatter_kernel(const PlanParams p)
+__global__ void __launch_bounds__(kPlanThreads) plan_kernel(const PlanParams p)
 {
-    extern __shared__ int32_t next[];
-    const int lane = threadIdx.x;
-    for (int e = lane; e < p.n_experts; e += 64) next[e] = p.counts[(int64_t)blockIdx.x * p.n_experts + e];
+    extern __shared__ int32_t next[];              // [wave][n_experts + 1], of no expert the last
+    __shared__ int32_t all[kMaxExperts], before[kMaxExperts], tile_at[kMaxExperts + 1];
+    __shared__ int2 sums[kPlanWaves];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = p.n_experts + 1;
+    for (int i = threadIdx.x; i < kPlanWaves * n; i += kPlanThreads) next[i] = 0;
+    all[threadIdx.x] = 0;
+    before[threadIdx.x] = 0;
     __syncthreads();
-    const int64_t first = (int64_t)blockIdx.x * kPlanChunk;
-    const int64_t end = first + kPlanChunk < p.n_pairs ? first + kPlanChunk : p.n_pairs;
+    const int64_t part_end = (blockIdx.x + 1) * p.per_part < p.n_pairs ? (blockIdx.x + 1) * p.per_part : p.n_pairs;
+    const int64_t first = blockIdx.x * p.per_part + wave * p.per_wave, end = first + p.per_wave < part_end ? first + p.per_wave : part_end;
+    int32_t *mine = next + wave * n;
+    for (int64_t at = first; at < end; at += 64) atomicAdd(&mine[expert_of(p.ids, at + lane, end, p.n_experts)], 1);
+    if (p.n_parts > 1) {                           // the workgroups' counts: of all, and of those before this one
+        const int e = threadIdx.x & ((1 << p.lg_lanes) - 1), step = kPlanThreads >> p.lg_lanes;
+        if (e < p.n_experts) {
+            int total = 0, lower = 0;
+#pragma unroll 8
+            for (int i = threadIdx.x >> p.lg_lanes; i < p.n_parts; i += step) {
+                const int c = p.counts[(int64_t)i * p.n_experts + e];
+                total += c;
+                lower += i < (int)blockIdx.x ? c : 0;
+            }
+            atomicAdd(&all[e], total);
+            atomicAdd(&before[e], lower);
+        }
+    }
+    __syncthreads();
+    const int e = threadIdx.x;
+    int count = 0;
+    if (e < p.n_experts) {
+        if (p.n_parts > 1) {
+            count = all[e];
+        } else {
+#pragma unroll
+            for (int w = 0; w < kPlanWaves; ++w) count += next[w * n + e];
+        }
+    }
+    const int tiles = (count + p.tile_rows - 1) / p.tile_rows;
+    int2 total;
+    const int2 start = scan_plan(make_int2(count, tiles), sums, total);
+    if (e < p.n_experts) {
+        all[e] = start.x;
+        tile_at[e] = start.y;
+        int at = start.x + (p.n_parts > 1 ? before[e] : 0);
+#pragma unroll
+        for (int w = 0; w < kPlanWaves; ++w) {
+            const int here = next[w * n + e];
+            next[w * n + e] = at;
+            at += here;
+        }
+        if (blockIdx.x == 0) p.offsets[e] = start.x;
+    }
+    if (e == 0) {
+        tile_at[p.n_experts] = total.y;
+        if (blockIdx.x == 0) p.offsets[p.n_experts] = total.x;
+    }
+    __syncthreads();
     for (int64_t at = first; at < end; at += 64) {
         const int id = expert_of(p.ids, at + lane, end, p.n_experts);
         const uint64_t same = same_id(id, p.bits);
-        const int before = __popcll(same & ((1ull << lane) - 1));
-        if (id < p.n_experts) p.order[next[id] + before] = (int32_t)(at + lane);
-        __syncthreads();
-        if (id < p.n_experts && before == 0) next[id] += __popcll(same);
-        __syncthreads();
+        const int earlier = __popcll(same & ((1ull << lane) - 1)), begin = mine[id];
+        if (id < p.n_experts) p.order[begin + earlier] = (int32_t)(at + lane);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if (earlier == 0) mine[id] = begin + __popcll(same);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
+    // the tiles, and what is behind the last pair, by all workgroups
+    for (int64_t i = blockIdx.x * (int64_t)kPlanThreads + threadIdx.x; i < p.n_tiles; i += (int64_t)p.n_parts * kPlanThreads) {
+        PlanTile t = {0, 0, 0, 0};
+        if (i < total.y) {
+            int lo = 0, hi = p.n_experts;          // the last expert that begins at or before tile i and has one
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (tile_at[mid] <= i) lo = mid;
+                else hi = mid;
+            }
+            const int expert_end = lo + 1 < p.n_experts ? all[lo + 1] : total.x;
+            t.expert = lo;
+            t.first = all[lo] + (int)(i - tile_at[lo]) * p.tile_rows;
+            t.count = expert_end - t.first < p.tile_rows ? expert_end - t.first : p.tile_rows;
+        }
+        p.tiles[i] = t;
+    }
+    for (int64_t i = total.x + blockIdx.x * (int64_t)kPlanThreads + threadIdx.x; i < p.n_pairs; i += (int64_t)p.n_parts * kPlanThreads) p.order[i] = -1;
 }
 
 // ---- the weighted sum
@@ -814,11 +862,13 @@ PlanParts plan_parts(int64_t n_pairs, int32_t n_experts)
     PlanParts q;
     q.tile_rows = plan_tile_rows(n_pairs, n_experts);
     q.n_tiles = plan_max_tiles(n_pairs, n_experts, q.tile_rows);
-    q.n_chunks = (n_pairs + kPlanChunk - 1) / kPlanChunk;
+    // workgroups of at least kPlanPart pairs, and no more than there are compute units
+    q.n_parts = std::max<int64_t>(1, std::min<int64_t>(256, n_pairs / kPlanPart));
+    q.per_wave = up((n_pairs + q.n_parts * kPlanWaves - 1) / (q.n_parts * kPlanWaves), 64);
     q.order = up(4 * ((int64_t)n_experts + 1), 256);
     q.tiles = up(q.order + 4 * n_pairs, 256);
     q.counts = up(q.tiles + (int64_t)sizeof(PlanTile) * q.n_tiles, 256);
-    q.total = up(q.counts + 4 * q.n_chunks * n_experts, 256);
+    q.total = up(q.counts + 4 * q.n_parts * n_experts, 256);
     return q;
 }
 
@@ -917,14 +967,15 @@ extern "C" int route_plan(const int32_t *ids_dev, int64_t n_pairs, int32_t n_exp
     p.n_pairs = n_pairs;
     p.n_experts = n_experts;
     p.bits = 32 - __builtin_clz((unsigned)n_experts);       // of 0 .. n_experts
-    p.n_chunks = (int32_t)q.n_chunks;
+    p.n_parts = (int32_t)q.n_parts;
+    p.per_wave = q.per_wave;
+    p.per_part = q.per_wave * kPlanWaves;
     p.tile_rows = q.tile_rows;
     p.n_tiles = (int32_t)q.n_tiles;
+    p.lg_lanes = 32 - __builtin_clz((unsigned)n_experts) - ((n_experts & (n_experts - 1)) == 0 ? 1 : 0);
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    const unsigned lds = 4 * ((unsigned)n_experts + 1);
-    if (n_pairs > 0) hipLaunchKernelGGL(plan_count_kernel, dim3((unsigned)q.n_chunks), dim3(64), lds, stream, p);
-    hipLaunchKernelGGL(plan_scan_kernel, dim3(1), dim3(kScanThreads), 0, stream, p);
-    if (n_pairs > 0) hipLaunchKernelGGL(plan_scatter_kernel, dim3((unsigned)q.n_chunks), dim3(64), lds, stream, p);
+    if (q.n_parts > 1) hipLaunchKernelGGL(plan_count_kernel, dim3((unsigned)q.n_parts), dim3(kPlanThreads), 4 * (unsigned)n_experts, stream, p);
+    hipLaunchKernelGGL(plan_kernel, dim3((unsigned)q.n_parts), dim3(kPlanThreads), 4 * kPlanWaves * ((unsigned)n_experts + 1), stream, p);
     return launched();
 }
 
