@@ -607,7 +607,15 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const PlanParams p)
     const int64_t part_end = (blockIdx.x + 1) * p.per_part < p.n_pairs ? (blockIdx.x + 1) * p.per_part : p.n_pairs;
     const int64_t first = blockIdx.x * p.per_part + wave * p.per_wave, end = first + p.per_wave < part_end ? first + p.per_wave : part_end;
     int32_t *mine = next + wave * n;
-    for (int64_t at = first; at < end; at += 64) atomicAdd(&mine[expert_of(p.ids, at + lane, end, p.n_experts)], 1);
+    // (four loads at a time, or a wave waits for each)
+    for (int64_t at = first; at < end; at += 256) {
+        int id[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) id[u] = expert_of(p.ids, at + 64 * u + lane, end, p.n_experts);
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (at + 64 * u < end) atomicAdd(&mine[id[u]], 1);
+    }
     if (p.n_parts > 1) {                           // the workgroups' counts: of all, and of those before this one
         const int e = threadIdx.x & ((1 << p.lg_lanes) - 1), step = kPlanThreads >> p.lg_lanes;
         if (e < p.n_experts) {
@@ -653,14 +661,20 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const PlanParams p)
         if (blockIdx.x == 0) p.offsets[p.n_experts] = total.x;
     }
     __syncthreads();
-    for (int64_t at = first; at < end; at += 64) {
-        const int id = expert_of(p.ids, at + lane, end, p.n_experts);
-        const uint64_t same = same_id(id, p.bits);
-        const int earlier = __popcll(same & ((1ull << lane) - 1)), begin = mine[id];
-        if (id < p.n_experts) p.order[begin + earlier] = (int32_t)(at + lane);
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        if (earlier == 0) mine[id] = begin + __popcll(same);
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    for (int64_t at = first; at < end; at += 256) {
+        int id[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) id[u] = expert_of(p.ids, at + 64 * u + lane, end, p.n_experts);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (at + 64 * u >= end) break;
+            const uint64_t same = same_id(id[u], p.bits);
+            const int earlier = __popcll(same & ((1ull << lane) - 1)), begin = mine[id[u]];
+            if (id[u] < p.n_experts) p.order[begin + earlier] = (int32_t)(at + 64 * u + lane);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            if (earlier == 0) mine[id[u]] = begin + __popcll(same);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        }
     }
     // the tiles, and what is behind the last pair, by all workgroups
     for (int64_t i = blockIdx.x * (int64_t)kPlanThreads + threadIdx.x; i < p.n_tiles; i += (int64_t)p.n_parts * kPlanThreads) {
