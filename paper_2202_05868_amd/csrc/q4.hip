@@ -9,7 +9,6 @@
 
 #include <algorithm>
 #include <cstdint>
-#include <cstdlib>
 #include <new>
 #include <type_traits>
 
@@ -775,16 +774,15 @@ Variant mid_variant(int waves)
     return {q4_mid_kernel<DT, CH, ZEROS, MT>, 32 * MT, 4, 64 * waves, std::max(x, std::max(halves, out))};
 }
 
-// The variant for `rows` rows of a tile of rows (16, 32 or 64).
+// The variant for `rows` rows of a tile of rows (16, 32 or 64): nt rows of tiles a workgroup (16 of more than 16 rows: the kernel for many workgroups).
 struct Choice {
-    int32_t rows, nt, waves;                           // nt: rows of tiles of a workgroup; 16: the kernel for many workgroups
-    bool few_steps = false;                            // 16 rows: nothing but the next step fetched ahead, and eight waves a SIMD
+    int32_t rows, nt, waves;
 };
 template <int DT, int CH, bool ZEROS>
 Variant mm_variant(const Choice &c)
 {
-    if (c.rows == 16 && c.few_steps) return split_variant<DT, CH, ZEROS, 2, 1, 1, 256>(4);
-    if (c.rows == 16) return c.nt == 1 ? split_variant<DT, CH, ZEROS, 1, 4, 2, 1024>(c.waves) : c.nt == 2 ? split_variant<DT, CH, ZEROS, 2, 4, 2, 1024>(c.waves) : split_variant<DT, CH, ZEROS, 4, 2, 2, 512>(c.waves);
+    if (c.rows == 16)
+        return c.nt == 1 ? split_variant<DT, CH, ZEROS, 1, 4, 2, 512>(c.waves) : c.nt == 2 ? split_variant<DT, CH, ZEROS, 2, 1, 1, 512>(c.waves) : split_variant<DT, CH, ZEROS, 4, 2, 2, 256>(c.waves);
     if (c.nt == 4) return c.rows == 32 ? mid_variant<DT, CH, ZEROS, 1>(c.waves) : mid_variant<DT, CH, ZEROS, 2>(c.waves);
     return c.rows == 32 ? Variant{q4_many_kernel<DT, CH, ZEROS, 1>, 32, 16, 256, 0} : Variant{q4_many_kernel<DT, CH, ZEROS, 2>, 64, 16, 256, 0};
 }
@@ -800,10 +798,13 @@ Variant mm_variant(int32_t group, bool zeros, const Choice &c)
 //   more than 16 rows: the kernel for many workgroups from 224 of them on (T 512, 4096 x 8192, 256 workgroups: 49, the other 55; T 192, 4096 x 14336, 168: 50 and
 //   46; T 256, 4096 x 8192, 128: 48 and 32); the other one with eight waves where a CU has one workgroup and each wave two steps (T 64, 8192 x 16384, 256
 //   workgroups: 34, with four 42; T 256, 4096 x 8192, 512: 39 and 32; T 57, 704 x 12878: 10.7 and 10.0)
-//   up to 16 rows: one row of tiles a workgroup while that is one for each CU (T 1, 4096 x 4096: 6.0, two 6.7; T 1, 8192 x 16384: 20.3 and 17.4), four for as
-//   many as two a CU and more rows of X than four, whose loads then cost (T 16, 8192 x 16384: 19.8, two 23.3; T 1: 19.2 and 17.4).  Where waves have up to four
-//   steps and there are two workgroups for each CU, they hide each other's waits better than loads far ahead do, which take registers (112 pairs of 28
-//   experts, 576 x 1024: 5.5, loads ahead 7.8; 64 pairs of 64 experts, 2048 x 2816: 30.6 and 31.8)
+//   up to 16 rows: one row of tiles a workgroup and W four steps ahead while that is one workgroup for each CU (T 1, 4096 x 4096: 5.2, two rows 6.1; T 1,
+//   8192 x 8192: 11.1 and 9.7).  Else two, and nothing ahead but the next step: then eight waves of a SIMD hide each other's waits (W four steps ahead
+//   takes registers for that; T 1, 8192 x 16384: 15.2 and 21.3; 112 pairs of 28 experts, 576 x 1024: 5.4 and 7.1).  Four rows of tiles, for which X is
+//   read half as often, with more than 8 rows of X and workgroups for every CU still (T 16, 8192 x 16384: 17.8, two 22.1; T 16, 4064 x 10999: 9.6 and 10.5; T 16,
+//   8192 x 8192, 512 rows of tiles: 14.6 and 12.0).
+//   Eight waves where each has two steps or workgroups are few (T 1, 2048 x 14336: 6.3, four 6.4; T 8, 8192 x 8192: 9.9 and 13.2; 8 pairs, 2048 x 1536: 7.0 and
+//   7.4), four where there are many (64 pairs of 64 experts, 2048 x 2816: 24.8, eight 25.5; 1408 x 2048: 14.9 and 16.2)
 Choice choose(const MmParams &p, int32_t rows, int64_t row_tiles, int64_t rows_each)
 {
     const int64_t tiles = row_tiles * p.tile_rows;
@@ -812,57 +813,8 @@ Choice choose(const MmParams &p, int32_t rows, int64_t row_tiles, int64_t rows_e
         return {rows, 4, row_tiles * ((p.tile_rows + 3) / 4) <= 256 && p.k_tiles >= 16 ? 8 : 4};
     }
     if (tiles <= 256 && !p.gated) return {16, 1, p.k_tiles >= 32 ? 8 : 4};
-    if (p.k_tiles <= 16 && tiles >= 1024) return {16, 2, 4, true};
-    if (tiles >= 512 && rows_each > 4) return {16, 4, p.k_tiles >= 16 ? 8 : 4};
-    return {16, 2, 4};
-}
-
-bool aligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
-
-int launched()
-{
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) {
-        set_last_hip_error((int)e);
-        return VBR_EHIP;
-    }
-    return VBR_OK;
-}
-
-// What both products ask of their operands; n_rows of Y
-int mm_args(const q4_t *h, const void *X_dev, int64_t ldx, const void *Y_dev, int64_t ldy, int32_t y_type, int64_t n_rows)
-{
-    if (!h || (y_type != VBR_F32 && y_type != h->dtype) || n_rows < 0) return VBR_EINVAL;
-    if (!h->dev) return VBR_ESTATE;
-    if (n_rows == 0) return VBR_OK;
-    if (!X_dev || !Y_dev || ldx < h->n_cols || ldx % 8 != 0 || ldy < h->rows() || !aligned(X_dev, 16) || !aligned(Y_dev, y_type == VBR_F32 ? 4 : 2)) return VBR_EINVAL;
-    return VBR_OK;
-}
-
-MmParams mm_params(const q4_t *h, const void *X_dev, int64_t ldx, int64_t x_rows, void *Y_dev, int64_t ldy, int64_t n_rows)
-{
-    MmParams p{};
-    const char *d = static_cast<const char *>(h->dev);
-    p.tiles = reinterpret_cast<const uint4v *>(d);
-    p.scales = d + h->scales_at();
-    p.zeros = d + h->zeros_at();
-    p.X = static_cast<const uint16_t *>(X_dev);
-    p.Y = Y_dev;
-    p.ldx = ldx;
-    p.ldy = ldy;
-    const int64_t x_bytes = b_bytes_of(x_rows, ldx, h->n_cols);
-    p.x_bytes = x_bytes <= kNearBytes ? (uint32_t)x_bytes : 0;
-    p.ldx_bytes = (uint32_t)(2 * ldx);
-    p.n_rows = n_rows;
-    p.k_tiles = h->k_tiles();
-    p.tile_rows = h->tile_rows();
-    p.steps = h->steps();
-    p.half = (int32_t)h->rows();
-    p.k_chunks = (int32_t)(h->n_cols / 32);
-    const uint32_t tiles_a_step = h->group <= 128 ? 1 : (uint32_t)h->group / 128;
-    p.step_divide = tiles_a_step == 1 ? 0 : (uint32_t)(((1ull << 32) + tiles_a_step - 1) / tiles_a_step);      // (tiles and tiles_a_step are below 2^16)
-    p.gated = h->gated;
-    return p;
+    if (tiles >= 640 && rows_each > 8) return {16, 4, 4};
+    return {16, 2, (p.k_tiles >= 16 && tiles < 2048) || (p.k_tiles >= 8 && tiles < 1024) ? 8 : 4};
 }
 
 void set_y(MmParams &p, int32_t y_type)
@@ -874,9 +826,7 @@ void set_y(MmParams &p, int32_t y_type)
 int launch_mm(const q4 *h, MmParams &p, int32_t rows, int64_t row_tiles, int64_t rows_each, void *hip_stream)
 {
     if (rows == 16 && p.x_bytes == 0) rows = 32;       // an X of 4 GiB and more: the other kernels have 64-bit addresses
-    Choice c = choose(p, rows, row_tiles, rows_each);
-    if (const char *e = getenv("Q4_NT")) c.nt = atoi(e);
-    if (const char *e = getenv("Q4_WAVES")) c.waves = atoi(e);
+    const Choice c = choose(p, rows, row_tiles, rows_each);
     const Variant v = h->dtype == VBR_F16 ? mm_variant<VBR_F16>(h->group, h->zeros, c) : mm_variant<VBR_BF16>(h->group, h->zeros, c);
     p.col_blocks = (int32_t)((p.tile_rows + v.tile_rows - 1) / v.tile_rows);
     p.by_col_blocks = Divide::by(p.col_blocks);

@@ -758,14 +758,23 @@ __global__ void __launch_bounds__(kRouteThreads) route_combine_kernel(const Comb
     float sum[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) sum[i] = 0.f;
-    for (int j = 0; j < p.top_k; ++j) {
-        const int64_t pair = row * p.top_k + j;
-        if ((uint32_t)p.ids[pair] >= (uint32_t)p.n_experts) continue;
-        const float w = p.weights[pair];
-        float x[8];
-        load8<TY>(p.y, pair * p.ldy + col, x);
+    // (four places' loads at a time; of a place that does not count, the first one's, without effect)
+    const int64_t first = row * p.top_k;
+    for (int j0 = 0; j0 < p.top_k; j0 += 4) {
+        bool there[4];
+        float w[4], x[4][8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum[i] = __builtin_fmaf(w, x[i], sum[i]);
+        for (int u = 0; u < 4; ++u) {
+            const int64_t pair = j0 + u < p.top_k ? first + j0 + u : first;
+            there[u] = (uint32_t)p.ids[pair] < (uint32_t)p.n_experts && j0 + u < p.top_k;
+            w[u] = p.weights[pair];
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) load8<TY>(p.y, (there[u] ? first + j0 + u : first) * p.ldy + col, x[u]);
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[i] = there[u] ? __builtin_fmaf(w[u], x[u][i], sum[i]) : sum[i];
     }
     store8<TO>(p.out, row * p.ldo + col, sum);
 }
