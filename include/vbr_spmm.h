@@ -370,6 +370,17 @@ int q4_mm_routed(const q4_t *h, const void *plan_dev, int64_t n_pairs, const voi
                  void *Y_dev, int64_t ldy, int32_t y_type, void *hip_stream);
 void q4_free(q4_t *h);
 
+/*
+ * A layer of experts in one call: out[row] = sum over its places of weights[pair] * (h[pair] D[expert]^T), h[pair] = gated product of X[row] with up's
+ * matrix of the expert, D those of down: route_plan, q4_mm_routed twice and route_combine in turn.  up is gated and gives as many columns as down takes,
+ * both have as many matrices and one dtype, and down's rows are a multiple of 8.  h is rounded to dtype, which the second product multiplies; its results stay in fp32 until
+ * they are summed.  Operands as in those calls; work_dev: caller-allocated, experts_work_bytes bytes (0 for sizes that do not fit), 256-byte
+ * aligned, of this call alone while it runs.  For one row the pairs are multiplied as they stand, without a plan.
+ */
+int64_t experts_work_bytes(const q4_t *up, const q4_t *down, int64_t n_rows, int32_t top_k);
+int experts_forward(const q4_t *up, const q4_t *down, const void *X_dev, int64_t ldx, int64_t n_rows, const int32_t *ids_dev,
+                    const float *weights_dev, int32_t top_k, void *out_dev, int64_t ldo, int32_t out_type, void *work_dev, void *hip_stream);
+
 const char *vbr_strerror(int code);
 int vbr_last_hip_error(void);   /* hipError_t of the last failing HIP call on this thread */
 

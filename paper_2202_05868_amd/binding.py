@@ -28,7 +28,8 @@ EXPORTS = ("sa1_reorder", "vbr_build", "vbr_get_index", "vbr_unpack_block", "vbr
            "vbr_last_hip_error", "sa1_blocking_curve", "csr_spmm_create", "csr_device_bytes", "csr_upload",
            "csr_spmm", "csr_free", "vbr_probe_launch", "vbr_get_launches", "vbr_audit", "vbr_get_tile_ksteps",
            "vbr_get_launch_functions", "route_topk", "route_topk_grad", "route_plan_bytes", "route_plan_order", "route_plan",
-           "route_combine", "route_combine_grad", "q4_create", "q4_device_bytes", "q4_upload", "q4_mm", "q4_mm_routed", "q4_free")
+           "route_combine", "route_combine_grad", "q4_create", "q4_device_bytes", "q4_upload", "q4_mm", "q4_mm_routed", "q4_free",
+           "experts_work_bytes", "experts_forward")
 
 
 class VbrError(RuntimeError):
@@ -103,9 +104,13 @@ def _load():
     lib.q4_upload.argtypes = [vp, vp, vp, vp, vp, vp]
     lib.q4_mm.argtypes = [vp, vp, i64, vp, i64, i32, i64, vp]
     lib.q4_mm_routed.argtypes = [vp, vp, i64, vp, i64, i64, vp, i64, i32, vp]
+    lib.experts_work_bytes.argtypes = [vp, vp, i64, i32]
+    lib.experts_work_bytes.restype = i64
+    lib.experts_forward.argtypes = [vp, vp, vp, i64, i64, vp, vp, i32, vp, i64, i32, vp, vp]
     lib.q4_free.argtypes = [vp]
     lib.q4_free.restype = None
-    for name in ("route_topk", "route_topk_grad", "route_plan", "route_combine", "route_combine_grad", "q4_create", "q4_upload", "q4_mm", "q4_mm_routed"):
+    for name in ("route_topk", "route_topk_grad", "route_plan", "route_combine", "route_combine_grad", "q4_create", "q4_upload", "q4_mm", "q4_mm_routed",
+                 "experts_forward"):
         getattr(lib, name).restype = ctypes.c_int
     for name in ("sa1_reorder", "vbr_build", "vbr_get_index", "vbr_unpack_block", "vbr_upload",
                  "vbr_spmm", "vbr_get_schedule", "sa1_blocking_curve", "csr_spmm_create", "csr_upload", "csr_spmm"):

@@ -118,6 +118,8 @@ struct MmParams {
     // routed, or null
     const PlanTile *plan_tiles;
     const int32_t *order;
+    const int32_t *ids;                        // or, of pairs that each have a tile of their own, these and how many matrices there are
+    int32_t n_mats;
     Divide by_places;                          // the pairs of a row of X
 };
 
@@ -217,10 +219,14 @@ __device__ __forceinline__ RowTile row_tile(const MmParams &p, int tile, int row
         const PlanTile t = p.plan_tiles[tile];
         return {t.expert, t.first, t.count};
     }
+    if (p.ids) {
+        const int32_t id = p.ids[tile];
+        return {id, tile, (uint32_t)id < (uint32_t)p.n_mats ? 1 : 0};
+    }
     const int64_t first = (int64_t)tile * rows, left = p.n_rows - first;
     return {0, first, (int32_t)(left < rows ? left : rows)};
 }
-__device__ __forceinline__ int64_t x_row(const MmParams &p, int64_t y_row) { return p.order ? (int64_t)p.by_places((uint32_t)y_row) : y_row; }
+__device__ __forceinline__ int64_t x_row(const MmParams &p, int64_t y_row) { return p.order || p.ids ? (int64_t)p.by_places((uint32_t)y_row) : y_row; }
 __device__ __forceinline__ uint32_t step_of(const MmParams &p, int t) { return p.step_divide ? __umulhi((uint32_t)t, p.step_divide) : (uint32_t)t; }
 
 // The steps of a wave among those that share the columns, begun at another one in every workgroup: rows of X and W are powers of two apart more often than
@@ -794,6 +800,54 @@ Variant mm_variant(int32_t group, bool zeros, const Choice &c)
     return zeros ? mm_variant<DT, 4, true>(c) : mm_variant<DT, 4, false>(c);
 }
 
+bool aligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+
+int launched()
+{
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) {
+        set_last_hip_error((int)e);
+        return VBR_EHIP;
+    }
+    return VBR_OK;
+}
+
+// What both products ask of their operands; n_rows of Y
+int mm_args(const q4_t *h, const void *X_dev, int64_t ldx, const void *Y_dev, int64_t ldy, int32_t y_type, int64_t n_rows)
+{
+    if (!h || (y_type != VBR_F32 && y_type != h->dtype) || n_rows < 0) return VBR_EINVAL;
+    if (!h->dev) return VBR_ESTATE;
+    if (n_rows == 0) return VBR_OK;
+    if (!X_dev || !Y_dev || ldx < h->n_cols || ldx % 8 != 0 || ldy < h->rows() || !aligned(X_dev, 16) || !aligned(Y_dev, y_type == VBR_F32 ? 4 : 2)) return VBR_EINVAL;
+    return VBR_OK;
+}
+
+MmParams mm_params(const q4_t *h, const void *X_dev, int64_t ldx, int64_t x_rows, void *Y_dev, int64_t ldy, int64_t n_rows)
+{
+    MmParams p{};
+    const char *d = static_cast<const char *>(h->dev);
+    p.tiles = reinterpret_cast<const uint4v *>(d);
+    p.scales = d + h->scales_at();
+    p.zeros = d + h->zeros_at();
+    p.X = static_cast<const uint16_t *>(X_dev);
+    p.Y = Y_dev;
+    p.ldx = ldx;
+    p.ldy = ldy;
+    const int64_t x_bytes = b_bytes_of(x_rows, ldx, h->n_cols);
+    p.x_bytes = x_bytes <= kNearBytes ? (uint32_t)x_bytes : 0;
+    p.ldx_bytes = (uint32_t)(2 * ldx);
+    p.n_rows = n_rows;
+    p.k_tiles = h->k_tiles();
+    p.tile_rows = h->tile_rows();
+    p.steps = h->steps();
+    p.half = (int32_t)h->rows();
+    p.k_chunks = (int32_t)(h->n_cols / 32);
+    const uint32_t tiles_a_step = h->group <= 128 ? 1 : (uint32_t)h->group / 128;
+    p.step_divide = tiles_a_step == 1 ? 0 : (uint32_t)(((1ull << 32) + tiles_a_step - 1) / tiles_a_step);      // (tiles and tiles_a_step are below 2^16)
+    p.gated = h->gated;
+    return p;
+}
+
 // By how many workgroups there would be for the 256 compute units, in us (bf16, groups of 128, T rows times K x N):
 //   more than 16 rows: the kernel for many workgroups from 224 of them on (T 512, 4096 x 8192, 256 workgroups: 49, the other 55; T 192, 4096 x 14336, 168: 50 and
 //   46; T 256, 4096 x 8192, 128: 48 and 32); the other one with eight waves where a CU has one workgroup and each wave two steps (T 64, 8192 x 16384, 256
@@ -915,21 +969,82 @@ extern "C" int q4_mm(const q4_t *h, const void *X_dev, int64_t ldx, void *Y_dev,
     return launch_mm(h, p, rows, (n_rows + rows - 1) / rows, n_rows, hip_stream);
 }
 
-extern "C" int q4_mm_routed(const q4_t *h, const void *plan_dev, int64_t n_pairs, const void *X_dev, int64_t ldx, int64_t n_rows, void *Y_dev, int64_t ldy, int32_t y_type, void *hip_stream)
+// plan_dev, or ids_dev: a tile for each pair
+static int mm_pairs(const q4_t *h, const void *plan_dev, const int32_t *ids_dev, int64_t n_pairs, const void *X_dev, int64_t ldx, int64_t n_rows, void *Y_dev, int64_t ldy, int32_t y_type,
+                    void *hip_stream)
 {
     const int rc = mm_args(h, X_dev, ldx, Y_dev, ldy, y_type, n_pairs);
     if (rc != VBR_OK) return rc;
     if (!plan_sizes_ok(n_pairs, (int32_t)h->n_mats)) return VBR_EUNSUPPORTED;
     if (n_pairs == 0) return VBR_OK;
-    if (!plan_dev || !aligned(plan_dev, 256) || n_rows < 1 || n_pairs % n_rows != 0) return VBR_EINVAL;
+    if (n_rows < 1 || n_pairs % n_rows != 0 || (!ids_dev && (!plan_dev || !aligned(plan_dev, 256)))) return VBR_EINVAL;
     MmParams p = mm_params(h, X_dev, ldx, n_rows, Y_dev, ldy, n_pairs);
+    p.by_places = Divide::by(n_pairs / n_rows);
+    set_y(p, y_type);
+    if (ids_dev) {
+        p.ids = ids_dev;
+        p.n_mats = (int32_t)h->n_mats;
+        return launch_mm(h, p, 16, n_pairs, 1, hip_stream);
+    }
     const PlanParts parts = plan_parts(n_pairs, (int32_t)h->n_mats);
     const char *d = static_cast<const char *>(plan_dev);
     p.order = reinterpret_cast<const int32_t *>(d + parts.order);
     p.plan_tiles = reinterpret_cast<const PlanTile *>(d + parts.tiles);
-    p.by_places = Divide::by(n_pairs / n_rows);
-    set_y(p, y_type);
     return launch_mm(h, p, parts.tile_rows, parts.n_tiles, n_pairs / h->n_mats, hip_stream);
+}
+
+extern "C" int q4_mm_routed(const q4_t *h, const void *plan_dev, int64_t n_pairs, const void *X_dev, int64_t ldx, int64_t n_rows, void *Y_dev, int64_t ldy, int32_t y_type, void *hip_stream)
+{
+    return mm_pairs(h, plan_dev, nullptr, n_pairs, X_dev, ldx, n_rows, Y_dev, ldy, y_type, hip_stream);
+}
+
+namespace {
+
+struct Work {
+    int64_t h, y, total;           // byte offsets in the work buffer, behind a plan
+};
+bool experts_ok(const q4_t *up, const q4_t *down, int64_t n_rows, int32_t top_k)
+{
+    if (!up || !down || !up->gated || down->gated || up->rows() != down->n_cols || up->n_mats != down->n_mats || up->dtype != down->dtype || down->n_rows % 8 != 0) return false;
+    return n_rows >= 0 && top_k >= 1 && top_k <= kMaxTopK && n_rows <= kMaxPairs / top_k;
+}
+Work experts_work(const q4_t *up, const q4_t *down, int64_t n_pairs)
+{
+    Work w;
+    w.h = plan_parts(n_pairs, (int32_t)up->n_mats).total;
+    w.y = (w.h + n_pairs * up->rows() * 2 + 255) / 256 * 256;
+    w.total = w.y + n_pairs * down->n_rows * 4;
+    return w;
+}
+
+}  // namespace
+
+extern "C" int64_t experts_work_bytes(const q4_t *up, const q4_t *down, int64_t n_rows, int32_t top_k)
+{
+    return experts_ok(up, down, n_rows, top_k) ? experts_work(up, down, n_rows * top_k).total : 0;
+}
+
+extern "C" int experts_forward(const q4_t *up, const q4_t *down, const void *X_dev, int64_t ldx, int64_t n_rows, const int32_t *ids_dev, const float *weights_dev, int32_t top_k,
+                               void *out_dev, int64_t ldo, int32_t out_type, void *work_dev, void *hip_stream)
+{
+    if (!experts_ok(up, down, n_rows, top_k)) return VBR_EINVAL;
+    if (!up->dev || !down->dev) return VBR_ESTATE;
+    if (n_rows == 0) return VBR_OK;
+    if (!ids_dev || !weights_dev || !out_dev || !work_dev || !aligned(work_dev, 256) || !aligned(ids_dev, 4) || !aligned(weights_dev, 4)) return VBR_EINVAL;
+    // (all that can be refused is, before anything is launched)
+    if ((out_type != VBR_F16 && out_type != VBR_BF16 && out_type != VBR_F32) || ldo < down->n_rows || ldo % 8 != 0 || !aligned(out_dev, 16)) return VBR_EINVAL;
+    const int64_t n_pairs = n_rows * top_k;
+    const Work w = experts_work(up, down, n_pairs);
+    char *d = static_cast<char *>(work_dev);
+    int rc = mm_args(up, X_dev, ldx, d + w.h, up->rows(), up->dtype, n_pairs);
+    if (rc != VBR_OK) return rc;
+    // One row needs no grouping: each of its pairs is a tile (the layer for one row, 8 of 128 experts of 2048 x 1536: 24.6 us with a plan).
+    const int32_t *direct = n_rows == 1 ? ids_dev : nullptr;
+    if (!direct) rc = route_plan(ids_dev, n_pairs, (int32_t)up->n_mats, work_dev, hip_stream);
+    if (rc == VBR_OK) rc = mm_pairs(up, work_dev, direct, n_pairs, X_dev, ldx, n_rows, d + w.h, up->rows(), up->dtype, hip_stream);
+    if (rc == VBR_OK) rc = mm_pairs(down, work_dev, direct, n_pairs, d + w.h, up->rows(), n_pairs, d + w.y, down->n_rows, VBR_F32, hip_stream);
+    if (rc == VBR_OK) rc = route_combine(d + w.y, down->n_rows, VBR_F32, ids_dev, weights_dev, n_rows, top_k, (int32_t)up->n_mats, down->n_rows, out_dev, ldo, out_type, hip_stream);
+    return rc;
 }
 
 extern "C" void q4_free(q4_t *h) { delete h; }

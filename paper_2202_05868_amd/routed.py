@@ -298,9 +298,24 @@ def experts_forward(x, ids, weights, up, down, out=None):
     matrices' type, which the second product multiplies; its results stay in float32 until they are summed."""
     if not up.gated or up.n_out != down.n_cols or up.n_mats != down.n_mats or down.gated or up.dtype is not down.dtype:
         raise ValueError("experts_forward: up must be gated, and down take what it gives, of as many experts and the same type")
-    plan = route_plan(ids, up.n_mats)
-    if x.shape[0] != plan.n_rows:
-        raise ValueError("experts_forward: x has %d rows, ids %d" % (x.shape[0], plan.n_rows))
-    h = up.mm_routed(x, plan)
-    y = down.mm_routed(h, plan, y_dtype=torch.float32)
-    return route_combine(y, ids, weights, out, out_dtype=x.dtype, n_experts=up.n_mats)
+    what = "experts_forward"
+    if ids.dim() != 2:
+        raise ValueError("%s: ids must be of shape (T, k)" % what)
+    n_rows, k = ids.shape
+    ldx = _rows(what, "x", x, n_rows, up.n_cols, (up.dtype,))
+    _dense(what, "ids", ids, ids.shape, torch.int32)
+    _dense(what, "weights", weights, ids.shape, torch.float32)
+    if out is None:
+        out = torch.empty((n_rows, down.n_out), dtype=x.dtype, device=x.device)
+    ldo = _rows(what, "out", out, n_rows, down.n_out, _TYPES)
+    if up._dev is None or down._dev is None:
+        raise VbrError(-4, what)
+    device = up._dev.get_device()
+    _together(what, device, down._dev, x, ids, weights, out)
+    n_bytes = int(_lib.experts_work_bytes(up._h, down._h, n_rows, k))
+    if n_bytes == 0:
+        raise VbrError(-1, what)
+    work = torch.empty(n_bytes, dtype=torch.uint8, device=x.device)
+    _call(what, _lib.experts_forward, device, up._h, down._h, x.data_ptr(), ldx, n_rows, ids.data_ptr(), weights.data_ptr(), k, out.data_ptr(), ldo,
+          _TYPES[out.dtype], work.data_ptr())
+    return out
