@@ -191,6 +191,75 @@ def test_choice_and_weights(case):
         assert np.all(np.abs(got - want) <= U * (2 * spread + 80) * want + 1e-37)
 
 
+def many_rows(seed, T, E, dtype):
+    """Scores of many rows, some so near each other that 32 bits do not tell their sums with a bias apart, some rows with closed experts or without any."""
+    gen = torch.Generator().manual_seed(seed)
+    l = 1.5 * torch.randn((T, E), generator=gen)
+    near = torch.rand((T, 1), generator=gen) < 0.2
+    l = torch.where(near, l[:, :1] * (1 + 1e-7 * torch.randint(-3, 4, (T, E), generator=gen)), l)
+    l = torch.where(torch.rand((T, E), generator=gen) < 0.05, torch.tensor(-math.inf), l)
+    l[T // 3: T // 3 + 3] = -math.inf
+    return l.to(TYPES[dtype])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [4095, 4096, 5001])
+@pytest.mark.parametrize("E,k,dtype,score,bias_step,groups,top_groups,renorm", [
+    (256, 8, "f32", "sigmoid", 2.0 ** -24, 8, 4, True), (256, 8, "f32", "softmax", 2.0 ** -26, 8, 3, False), (128, 8, "bf16", "softmax", None, 1, 1, True),
+    (240, 10, "f16", "sigmoid", 0.1, 8, 5, True), (16, 3, "f32", "softmax", None, 4, 2, False), (100, 16, "bf16", "sigmoid", 0.0, 1, 1, False), (60, 1, "f32", "sigmoid", None, 1, 1, True),
+    (33, 5, "f16", "softmax", 2.0 ** -20, 3, 2, True), (256, 4, "bf16", "sigmoid", 0.1, 16, 16, True)])
+def test_choice_of_many_rows(T, E, k, dtype, score, bias_step, groups, top_groups, renorm):
+    l = many_rows(E, T, E, dtype)
+    bias = None if bias_step is None else bias_step * torch.randn(E, generator=torch.Generator().manual_seed(E))
+    ids, weights = routed.route_topk(l.to(DEV), k, score=score, bias=None if bias is None else bias.to(DEV), n_groups=groups, top_groups=top_groups, renormalise=renorm, scale=1.5)
+    # the definition, all rows at once
+    x = np64(l)
+    closed = x == -np.inf
+    if score == "softmax":
+        most = x.max(1, keepdims=True)
+        e = np.exp(x - np.where(most == -np.inf, 0, most))
+        s = e / np.maximum(e.sum(1, keepdims=True), 1e-300)
+    else:
+        s = np.where(closed, 0, 1 / (1 + np.exp(-x)))
+    key = s + (0 if bias is None else np64(bias))
+    out = closed.copy()
+    if groups > 1:
+        by = -np.sort(-np.where(closed, -np.inf, key).reshape(T, groups, -1), 2)[:, :, :2]
+        total = by[:, :, 0] + np.where(by[:, :, -1] == -np.inf, 0, by[:, :, -1]) * (by.shape[2] > 1)
+        stays = np.argsort(-total, 1, kind="stable")[:, :top_groups]
+        mask = np.zeros((T, groups), bool)
+        np.put_along_axis(mask, stays, True, 1)
+        out |= ~np.repeat(mask, E // groups, 1)
+    order = x if bias is None else key
+    want = np.argsort(-np.where(out, -np.inf, order), 1, kind="stable")[:, :k]
+    want = np.where(np.take_along_axis(out, want, 1), -1, want)
+    assert np.array_equal(ids.cpu().numpy(), want)
+    w = np.where(want >= 0, np.take_along_axis(s, np.maximum(want, 0), 1), 0)
+    if renorm:
+        w = w / np.maximum(w.sum(1, keepdims=True), 1e-300)
+    spread = np.where(closed, 0, np.abs(x)).max(1, keepdims=True) * 2
+    assert np.all(np.abs(np64(weights) - 1.5 * w) <= U * (2 * spread + 80) * 1.5 * w)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,E,k,dtype,score,renorm", [(4096, 128, 8, "bf16", "softmax", True), (5001, 256, 16, "f32", "sigmoid", True), (4500, 60, 3, "f16", "softmax", False), (4099, 130, 2, "f32", "sigmoid", False)])
+def test_gradient_of_many_rows(T, E, k, dtype, score, renorm):
+    l = many_rows(E, T, E, dtype)
+    gen = torch.Generator().manual_seed(2)
+    ids = torch.randint(-1, E + 1, (T, k), generator=gen, dtype=torch.int32)
+    dw = torch.randn((T, k), generator=gen)
+    got = np64(routed.route_topk_grad(l.to(DEV), ids.to(DEV), dw.to(DEV), score=score, renormalise=renorm, scale=1.5))
+    rows = np.r_[0:40, T // 3 - 2: T // 3 + 6, T - 40: T]
+    l64, i64, d64 = np64(l)[rows], ids.numpy().astype(np.int64)[rows], np64(dw)[rows]
+    want = choice_grad(l64, i64, d64, score, renorm, 1.5)
+    # every term of the gradient is at most 1.5 |dw| (weights and their derivatives are at most 1)
+    limit = U * 400 * 1.5 * np.abs(d64).sum(1, keepdims=True)
+    assert np.all(np.abs(got[rows] - want) <= limit + half_step(l.dtype) * (np.abs(want) + limit) + (2.0 ** -25 if dtype == "f16" else 0))
+    other = torch.from_numpy(rows)
+    few = routed.route_topk_grad(l[other].to(DEV), ids[other].to(DEV), dw[other].to(DEV), score=score, renormalise=renorm, scale=1.5)
+    assert np.all(np.abs(np64(few) - got[rows]) <= 2 * (limit + half_step(l.dtype) * (np.abs(want) + limit) + (2.0 ** -25 if dtype == "f16" else 0)))
+
+
 def test_gradient_of_the_choice_is_the_difference_quotient():
     rng = np.random.default_rng(3)
     for score in ("softmax", "sigmoid"):
@@ -251,7 +320,7 @@ def test_gradient_of_the_choice(T, E, k, dtype, score, renorm):
 
 
 # ------------------------------------------------------------------------------------------- the grouping
-PLANS = [(1, 1, 1), (1, 4, 7), (5, 3, 64), (64, 1, 1), (100, 8, 256), (257, 6, 60), (4096, 2, 1024), (3000, 8, 5), (0, 2, 8), (20000, 4, 300)]
+PLANS = [(1, 1, 1), (4097, 2, 1000), (70000, 2, 17), (1023, 4, 3), (1, 4, 7), (5, 3, 64), (64, 1, 1), (100, 8, 256), (257, 6, 60), (4096, 2, 1024), (3000, 8, 5), (0, 2, 8), (20000, 4, 300)]
 
 
 @pytest.mark.gpu
@@ -295,8 +364,26 @@ MM = [
 ]
 
 
+# as many rows and outputs as fill the GPU
+MM_FULL = [
+    (1000, 3600, 32, 32, "f16", True, False),
+    (900, 4098, 160, 64, "bf16", False, True),
+    (961, 3700, 288, 128, "bf16", True, False),
+    (1024, 3585, 416, 256, "f16", False, False),
+    (31, 57400, 96, 32, "bf16", False, False),
+    (20, 57360, 320, 64, "f16", True, True),
+    (32, 57344, 640, 128, "bf16", True, False),
+    (700, 6000, 256, 32, "bf16", True, True),
+    (16, 20000, 1100 // 32 * 32, 128, "f16", True, False),
+    (10, 12000, 2304, 64, "bf16", True, True),
+    (3, 33000, 576, 32, "bf16", False, False),
+    (64, 16384, 2048, 128, "f16", False, False),
+    (100, 9000, 160, 64, "bf16", True, False),
+]
+
+
 @pytest.mark.gpu
-@pytest.mark.parametrize("case", MM, ids=lambda c: "T%d-N%d-K%d-g%d-%s-z%d-gated%d" % c)
+@pytest.mark.parametrize("case", MM + MM_FULL, ids=lambda c: "T%d-N%d-K%d-g%d-%s-z%d-gated%d" % c)
 @pytest.mark.parametrize("out", ["same", "f32"])
 def test_products_with_one_matrix(case, out):
     T, N, K, group, dtype, zeros, gate = case
@@ -330,6 +417,11 @@ ROUTED = [
     (513, 1, 2, 32, 1024, 32, "bf16", True, False),
     (40, 8, 130, 20, 96, 32, "f16", True, False),
     (600, 4, 8, 258, 544, 128, "bf16", True, True),
+    (400, 4, 64, 1026, 160, 32, "f16", True, True),
+    (2000, 4, 64, 514, 288, 128, "bf16", True, False),
+    (2000, 4, 64, 514, 224, 64, "f16", False, True),
+    (250, 4, 60, 700, 160, 64, "bf16", False, False),
+    (60, 4, 40, 2064, 800, 64, "bf16", False, False),
 ]
 
 
