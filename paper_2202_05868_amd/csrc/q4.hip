@@ -44,12 +44,12 @@ namespace {
 struct PackParams {
     const uint8_t *codes, *zeros;
     const uint16_t *scales;
-    uint32_t *tiles;
+    uint4v *tiles;
     uint16_t *kept_scales;
     uint8_t *kept_zeros;
-    int64_t n_words, n_kept;
+    int64_t n_tiles, n_kept;
     int64_t n_rows, half, n_cols, tile_rows, k_tiles, groups, steps;
-    int32_t gated, rotate, groups_a_step;
+    int32_t gated, rotate, groups_a_step, words;      // words: rows of codes can be read 4 bytes at a time only
 };
 
 __device__ __forceinline__ int64_t source_row(const PackParams &p, int64_t tile_row, int n)       // in its matrix; -1: none
@@ -58,49 +58,71 @@ __device__ __forceinline__ int64_t source_row(const PackParams &p, int64_t tile_
     return in_half < p.half ? in_half + (p.gated && (tile_row & 1) ? p.half : 0) : -1;
 }
 
+// A wave turns tiles one after the other: lane 16 j + n reads the codes of columns 32 j .. 32 j + 31 of row n, four words, and the lanes of a row exchange
+// them, so that lane 16 q + n has word q of each.
+constexpr int kPackTiles = 8;          // of a wave
 __global__ void __launch_bounds__(256) q4_pack_codes_kernel(const PackParams p)
 {
-    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (at >= p.n_words) return;
-    const int i = at & 3, n = at >> 2 & 15, q = at >> 6 & 3;
-    const int64_t tile = at >> 8, t = tile % p.k_tiles, row_of_all = tile / p.k_tiles, mat = row_of_all / p.tile_rows;
-    const int64_t row = source_row(p, row_of_all - mat * p.tile_rows, n), k = t * 128 + 32 * i + 8 * q;
-    uint32_t word = 0;
-    if (row >= 0 && k < p.n_cols) {
-        const uint32_t codes = *reinterpret_cast<const uint32_t *>(p.codes + (mat * p.n_rows + row) * (p.n_cols / 2) + k / 2);
+    const int lane = threadIdx.x & 63, n = lane & 15, j = lane >> 4;
+    const int64_t first = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * kPackTiles;
+    int64_t row_of_all = first / p.k_tiles, t = first - row_of_all * p.k_tiles, mat = row_of_all / p.tile_rows, tile_row = row_of_all - mat * p.tile_rows;
+    for (int64_t tile = first; tile < first + kPackTiles && tile < p.n_tiles; ++tile) {
+        const int64_t row = source_row(p, tile_row, n), k = t * 128 + 32 * j;
+        uint4v w = {0, 0, 0, 0};
+        if (row >= 0 && k < p.n_cols) {
+            const uint8_t *src = p.codes + (mat * p.n_rows + row) * (p.n_cols / 2) + k / 2;
+            if (p.words) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) word |= (codes >> 8 * j & 15u) << 4 * j | (codes >> (8 * j + 4) & 15u) << (4 * j + 16);
+                for (int i = 0; i < 4; ++i) w[i] = reinterpret_cast<const uint32_t *>(src)[i];
+            } else {
+                w = *reinterpret_cast<const uint4v *>(src);
+            }
+        }
+        auto swap = [](auto a, auto b, auto f, uint4v &w) {
+            const auto r = f(w[a.value], w[b.value]);
+            w[a.value] = (uint32_t)r[0];
+            w[b.value] = (uint32_t)r[1];
+        };
+        const auto far = [](uint32_t a, uint32_t b) { return __builtin_amdgcn_permlane32_swap(a, b, false, false); };
+        const auto near = [](uint32_t a, uint32_t b) { return __builtin_amdgcn_permlane16_swap(a, b, false, false); };
+        swap(constant<0>(), constant<2>(), far, w);
+        swap(constant<1>(), constant<3>(), far, w);
+        swap(constant<0>(), constant<1>(), near, w);
+        swap(constant<2>(), constant<3>(), near, w);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t codes = w[i];
+            uint32_t word = 0;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) word |= (codes >> 8 * u & 15u) << 4 * u | (codes >> (8 * u + 4) & 15u) << (4 * u + 16);
+            w[i] = word << p.rotate | word >> (32 - p.rotate);
+        }
+        p.tiles[tile * 64 + lane] = w;
+        if (++t == p.k_tiles) {
+            t = 0;
+            if (++tile_row == p.tile_rows) {
+                tile_row = 0;
+                ++mat;
+            }
+        }
     }
-    p.tiles[at] = word << p.rotate | word >> (32 - p.rotate);
 }
 
 __global__ void __launch_bounds__(256) q4_pack_scales_kernel(const PackParams p)
 {
-    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (at >= p.n_kept) return;
-    const int in_step = (int)(at % p.groups_a_step);
-    const int64_t of_step = at / p.groups_a_step;
-    const int n = of_step & 15;
-    const int64_t g = (of_step >> 4) % p.steps * p.groups_a_step + in_step, row_of_all = (of_step >> 4) / p.steps, mat = row_of_all / p.tile_rows;
-    const int64_t row = source_row(p, row_of_all - mat * p.tile_rows, n), from = (mat * p.n_rows + row) * p.groups + g;
-    const bool there = row >= 0 && g < p.groups;
-    p.kept_scales[at] = there ? p.scales[from] : 0;
-    if (p.kept_zeros) p.kept_zeros[at] = there ? p.zeros[from] : 0;
+    for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < p.n_kept; at += (int64_t)gridDim.x * 256) {
+        const int in_step = (int)(at % p.groups_a_step);
+        const int64_t of_step = at / p.groups_a_step;
+        const int n = of_step & 15;
+        const int64_t g = (of_step >> 4) % p.steps * p.groups_a_step + in_step, row_of_all = (of_step >> 4) / p.steps, mat = row_of_all / p.tile_rows;
+        const int64_t row = source_row(p, row_of_all - mat * p.tile_rows, n), from = (mat * p.n_rows + row) * p.groups + g;
+        const bool there = row >= 0 && g < p.groups;
+        p.kept_scales[at] = there ? p.scales[from] : 0;
+        if (p.kept_zeros) p.kept_zeros[at] = there ? p.zeros[from] : 0;
+    }
 }
 
 // ---- the products
-
-// i / d for i below 2^31: 2^(31 + l) / d rounded up, l the bits of d - 1, times i
-struct Divide {
-    uint32_t factor;
-    int32_t shift;
-    static Divide by(int64_t d)
-    {
-        const int l = d > 1 ? 64 - __builtin_clzll((unsigned long long)d - 1) : 0;
-        return {(uint32_t)(((1ull << (31 + l)) + d - 1) / d), 31 + l};
-    }
-    __device__ __forceinline__ uint32_t operator()(uint32_t i) const { return (uint32_t)((uint64_t)i * factor >> shift); }
-};
 
 struct MmParams {
     const uint4v *tiles;
@@ -886,7 +908,7 @@ int launch_mm(const q4 *h, MmParams &p, int32_t rows, int64_t row_tiles, int64_t
     p.by_col_blocks = Divide::by(p.col_blocks);
     p.lg_waves = __builtin_ctz(v.threads / 64);
     const int64_t grid = row_tiles * p.col_blocks;
-    if (grid > INT32_MAX) return VBR_EUNSUPPORTED;
+    if (grid > kMostThreads / v.threads || grid > INT32_MAX) return VBR_EUNSUPPORTED;
     hipLaunchKernelGGL(v.kernel, dim3((unsigned)grid), dim3(v.threads), v.lds, static_cast<hipStream_t>(hip_stream), p);
     return launched();
 }
@@ -927,10 +949,11 @@ extern "C" int q4_upload(q4_t *h, const void *codes_dev, const void *scales_dev,
     p.codes = static_cast<const uint8_t *>(codes_dev);
     p.scales = static_cast<const uint16_t *>(scales_dev);
     p.zeros = static_cast<const uint8_t *>(zeros_dev);
-    p.tiles = reinterpret_cast<uint32_t *>(d);
+    p.tiles = reinterpret_cast<uint4v *>(d);
     p.kept_scales = reinterpret_cast<uint16_t *>(d + h->scales_at());
     p.kept_zeros = h->zeros ? reinterpret_cast<uint8_t *>(d + h->zeros_at()) : nullptr;
-    p.n_words = h->scales_at() / 4;
+    p.n_tiles = h->scales_at() / 1024;
+    p.words = !aligned(codes_dev, 16);
     p.n_kept = h->kept();
     p.n_rows = h->n_rows;
     p.half = h->rows();
@@ -942,10 +965,11 @@ extern "C" int q4_upload(q4_t *h, const void *codes_dev, const void *scales_dev,
     p.groups_a_step = h->groups_a_step();
     p.gated = h->gated;
     p.rotate = h->dtype == VBR_F16 ? 6 : 3;
-    if ((p.n_words + 255) / 256 > INT32_MAX) return VBR_EUNSUPPORTED;
+    const int64_t workgroups = (p.n_tiles + 4 * kPackTiles - 1) / (4 * kPackTiles);
+    if (workgroups > kMostThreads / 256) return VBR_EUNSUPPORTED;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    hipLaunchKernelGGL(q4_pack_codes_kernel, dim3((unsigned)((p.n_words + 255) / 256)), dim3(256), 0, stream, p);
-    hipLaunchKernelGGL(q4_pack_scales_kernel, dim3((unsigned)((p.n_kept + 255) / 256)), dim3(256), 0, stream, p);
+    hipLaunchKernelGGL(q4_pack_codes_kernel, dim3((unsigned)workgroups), dim3(256), 0, stream, p);
+    hipLaunchKernelGGL(q4_pack_scales_kernel, dim3((unsigned)std::min<int64_t>((p.n_kept + 255) / 256, 1 << 20)), dim3(256), 0, stream, p);
     const int rc = launched();
     if (rc != VBR_OK) return rc;
     const hipError_t e = hipStreamSynchronize(stream);

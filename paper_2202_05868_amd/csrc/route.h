@@ -1,6 +1,8 @@
 // The layout of a plan (route_plan), which the routed products read.
 #pragma once
 
+#include <hip/hip_runtime.h>
+
 #include <cstdint>
 
 #include "vbr_spmm.h"
@@ -11,6 +13,20 @@ constexpr int32_t kMaxExperts = 1024;              // one thread of a workgroup 
 constexpr int32_t kMaxTopK = 64, kMaxGroups = 64;  // one lane each
 constexpr int64_t kMaxPairs = 1 << 30;             // positions are 32 bits
 constexpr int64_t kPlanPart = 4096;                // pairs of a workgroup, at least, where there are several
+
+constexpr int64_t kMostThreads = 0xFFFFFFFFll;     // of a launch
+
+// i / d for i below 2^31: 2^(31 + l) / d rounded up, l the bits of d - 1, times i
+struct Divide {
+    uint32_t factor;
+    int32_t shift;
+    static Divide by(int64_t d)
+    {
+        const int l = d > 1 ? 64 - __builtin_clzll((unsigned long long)d - 1) : 0;
+        return {(uint32_t)(((1ull << (31 + l)) + d - 1) / d), 31 + l};
+    }
+    __host__ __device__ uint32_t operator()(uint32_t i) const { return (uint32_t)((uint64_t)i * factor >> shift); }
+};
 
 // Byte offsets in a plan: int32 offsets [n_experts + 1] at 0, int32 order [n_pairs], PlanTile tiles [n_tiles],
 // int32 counts [n_parts][n_experts].

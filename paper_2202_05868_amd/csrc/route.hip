@@ -705,6 +705,7 @@ struct CombineParams {
     float *dweights;
     int64_t ldy, ldo, lddy, n_rows;
     int32_t n_cols, top_k, n_experts, n_chunks;
+    Divide by_chunks;
 };
 
 template <int TY>
@@ -747,32 +748,31 @@ __device__ __forceinline__ void store8(void *p, int64_t i, const float (&x)[8])
     }
 }
 
-// A thread owns eight columns of a row of out; the row's results are added in the order of their places.
-template <int TY, int TO>
+// A thread owns eight columns of a row of out; the row's results are added in the order of their places.  Bound by what it reads; AT places are on
+// their way at a time (of one that does not count, the first one's, without effect).
+template <int TY, int TO, int AT>
 __global__ void __launch_bounds__(kRouteThreads) route_combine_kernel(const CombineParams p)
 {
-    const int64_t at = (int64_t)blockIdx.x * kRouteThreads + threadIdx.x;
-    const int64_t row = at / p.n_chunks;
-    const int col = (int)(at - row * p.n_chunks) * 8;
+    const uint32_t at = blockIdx.x * (uint32_t)kRouteThreads + threadIdx.x, row = p.by_chunks(at);
+    const int col = (int)(at - row * (uint32_t)p.n_chunks) * 8;
     if (row >= p.n_rows) return;
     float sum[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) sum[i] = 0.f;
-    // (four places' loads at a time; of a place that does not count, the first one's, without effect)
-    const int64_t first = row * p.top_k;
-    for (int j0 = 0; j0 < p.top_k; j0 += 4) {
-        bool there[4];
-        float w[4], x[4][8];
+    const int64_t first = (int64_t)row * p.top_k;
+    for (int j0 = 0; j0 < p.top_k; j0 += AT) {
+        bool there[AT];
+        float w[AT], x[AT][8];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
+        for (int u = 0; u < AT; ++u) {
             const int64_t pair = j0 + u < p.top_k ? first + j0 + u : first;
             there[u] = (uint32_t)p.ids[pair] < (uint32_t)p.n_experts && j0 + u < p.top_k;
             w[u] = p.weights[pair];
         }
 #pragma unroll
-        for (int u = 0; u < 4; ++u) load8<TY>(p.y, (there[u] ? first + j0 + u : first) * p.ldy + col, x[u]);
+        for (int u = 0; u < AT; ++u) load8<TY>(p.y, (there[u] ? first + j0 + u : first) * p.ldy + col, x[u]);
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
+        for (int u = 0; u < AT; ++u)
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum[i] = there[u] ? __builtin_fmaf(w[u], x[u][i], sum[i]) : sum[i];
     }
@@ -930,7 +930,9 @@ extern "C" int route_topk(const vbr_route_t *how, const void *logits_dev, int64_
     const Width width = route_width(how->n_experts, how->top_k, how->n_groups, n_rows);
     const int32_t lanes_a_group = p.group_size / width.each;
     p.lanes_a_group = p.group_size % width.each == 0 && lanes_a_group <= 8 && (lanes_a_group & (lanes_a_group - 1)) == 0 ? lanes_a_group : 0;
-    const unsigned grid = (unsigned)((n_rows + kRouteThreads / width.lanes - 1) / (kRouteThreads / width.lanes));
+    const int64_t workgroups = (n_rows + kRouteThreads / width.lanes - 1) / (kRouteThreads / width.lanes);
+    if (workgroups > kMostThreads / kRouteThreads) return VBR_EUNSUPPORTED;
+    const unsigned grid = (unsigned)workgroups;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     ROUTE_BY_TYPE(route_topk_kernel, logits_type);
     return launched();
@@ -960,7 +962,9 @@ extern "C" int route_topk_grad(const vbr_route_t *how, const void *logits_dev, i
     p.whole = whole_pieces(logits_dev, ld, size);
     p.whole_out = whole_pieces(dlogits_dev, ldd, size);
     const Width width = route_width(how->n_experts, how->top_k, 1, n_rows);
-    const unsigned grid = (unsigned)((n_rows + kRouteThreads / width.lanes - 1) / (kRouteThreads / width.lanes));
+    const int64_t workgroups = (n_rows + kRouteThreads / width.lanes - 1) / (kRouteThreads / width.lanes);
+    if (workgroups > kMostThreads / kRouteThreads) return VBR_EUNSUPPORTED;
+    const unsigned grid = (unsigned)workgroups;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     ROUTE_BY_TYPE(route_topk_grad_kernel, logits_type);
     return launched();
@@ -1013,6 +1017,13 @@ int combine_args(int32_t y_type, int32_t out_type, int64_t n_cols, int64_t n_row
     return VBR_OK;
 }
 
+template <int TY, int TO>
+constexpr auto route_combine_2 = route_combine_kernel<TY, TO, 2>;
+template <int TY, int TO>
+constexpr auto route_combine_4 = route_combine_kernel<TY, TO, 4>;
+template <int TY, int TO>
+constexpr auto route_combine_8 = route_combine_kernel<TY, TO, 8>;
+
 #define COMBINE_LAUNCH(KERNEL, TY, TO) hipLaunchKernelGGL((KERNEL<TY, TO>), dim3((unsigned)grid), dim3(kRouteThreads), 0, stream, p)
 #define COMBINE_BY_OUT(KERNEL, TY)                                      \
     do {                                                                \
@@ -1049,10 +1060,13 @@ extern "C" int route_combine(const void *y_dev, int64_t ldy, int32_t y_type, con
     p.top_k = top_k;
     p.n_experts = n_experts;
     p.n_chunks = (int32_t)(n_cols / 8);
+    p.by_chunks = Divide::by(p.n_chunks);
     const int64_t grid = (n_rows * p.n_chunks + kRouteThreads - 1) / kRouteThreads;
-    if (grid > INT32_MAX) return VBR_EUNSUPPORTED;
+    if (grid > kMostThreads / 2 / kRouteThreads) return VBR_EUNSUPPORTED;          // (threads are divided by n_chunks in 31 bits)
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    COMBINE_BY_TYPES(route_combine_kernel);
+    if (top_k <= 2) COMBINE_BY_TYPES(route_combine_2);
+    else if (top_k <= 4) COMBINE_BY_TYPES(route_combine_4);
+    else COMBINE_BY_TYPES(route_combine_8);
     return launched();
 }
 
@@ -1080,6 +1094,7 @@ extern "C" int route_combine_grad(const void *dout_dev, int64_t ldo, int32_t out
     p.top_k = top_k;
     p.n_experts = n_experts;
     const int64_t grid = (n_rows * top_k + kRouteThreads / 64 - 1) / (kRouteThreads / 64);
+    if (grid > kMostThreads / kRouteThreads) return VBR_EUNSUPPORTED;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     COMBINE_BY_TYPES(route_combine_grad_kernel);
     return launched();

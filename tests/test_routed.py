@@ -491,6 +491,41 @@ def test_matrices_beyond_4_gib(count):
         assert_close(y[r: r + 1, rows], want, tol, torch.float32)
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [3, 20])
+def test_rows_of_x_beyond_4_gib(T):
+    K, N, ld = 256, 40, 2 ** 31 // T // 8 * 8 + 64                           # T rows that span more than 2^31 elements
+    gen = torch.Generator().manual_seed(T)
+    q = matrices(gen, 3, N, K, 64, torch.bfloat16, True)
+    far = torch.empty(T * ld, dtype=torch.bfloat16, device=DEV).as_strided((T, K), (ld, 1))
+    x = torch.randn((T, K), generator=gen).to(torch.bfloat16)
+    far.copy_(x.to(DEV))
+    m = routed.Q4(*[a.to(DEV) for a in q], group=64).upload()
+    ids = torch.arange(T, dtype=torch.int32).view(T, 1) % 3
+    y = m.mm_routed(far, routed.route_plan(ids.to(DEV), 3), y_dtype=torch.float32)
+    one = routed.Q4(*[a[0].to(DEV) for a in q], group=64).upload()
+    y0 = one.mm(far, y_dtype=torch.float32)
+    for r in range(T):
+        want, tol = product(np64(x[r: r + 1]), q, r % 3, 64)
+        assert_close(y[r: r + 1], want, tol, torch.float32)
+    want, tol = product(np64(x), q, 0, 64)
+    assert_close(y0, want, tol, torch.float32)
+
+
+@pytest.mark.gpu
+def test_codes_that_begin_between_words():
+    gen = torch.Generator().manual_seed(8)
+    q = matrices(gen, 1, 50, 160, 32, torch.float16, True)
+    raw = torch.zeros(50 * 80 + 16, dtype=torch.uint8, device=DEV)
+    x = torch.randn((4, 160), generator=gen).half()
+    want, tol = product(np64(x), q, 0, 32)
+    for shift in (0, 1, 4, 8):
+        codes = raw[shift: shift + 50 * 80].view(50, 80)
+        codes.copy_(q[0][0].to(DEV))
+        m = routed.Q4(codes, q[1][0].to(DEV), q[2][0].to(DEV), group=32).upload()
+        assert_close(m.mm(x.to(DEV), y_dtype=torch.float32), want, tol, torch.float32)
+
+
 # ------------------------------------------------------------------------------------------- the sum
 SUMS = [(1, 1, 8, "f32", "f32"), (3, 4, 72, "bf16", "bf16"), (33, 8, 520, "f16", "f16"), (7, 2, 4096, "f32", "bf16"), (5, 3, 1000, "f32", "f16"), (130, 6, 64, "bf16", "f32"),
         (2, 64, 256, "bf16", "bf16"), (1000, 5, 24, "f16", "f32")]
