@@ -359,7 +359,7 @@ int route_combine_grad(const void *dout_dev, int64_t ldo, int32_t out_type, cons
  *               of which n_pairs must be a multiple: pair p meets row p / (n_pairs / n_rows) (n_pairs rows: a row for each pair).
  * X: dtype, ldx >= n_cols, ldx % 8 == 0, 16-byte aligned.  Y: fp32 (VBR_F32) or dtype, any ldy >= its columns.  Weights are not rounded: codes are multiplied as
  * they are on the matrix units, and scales and zero points applied to sums, in fp32; with y_type = dtype a result is rounded once.  A NaN or Inf
- * in a row of X stays in that row's results.
+ * in a row of X stays in that row's results, all of which may be NaN then; sums of (16 + code) x have to fit into fp32.
  */
 typedef struct q4 q4_t;
 int q4_create(int64_t n_mats, int64_t n_rows, int64_t n_cols, int32_t group, int32_t dtype, int32_t zeros, int32_t gated, q4_t **out);

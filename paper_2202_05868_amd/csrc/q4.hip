@@ -296,9 +296,6 @@ __device__ __forceinline__ float sum_over_quarters(float x)           // of lane
     return __builtin_bit_cast(float, (uint32_t)b[0]) + __builtin_bit_cast(float, (uint32_t)b[1]);
 }
 
-// ---- few workgroups' worth of rows: 16 MT rows of X times NT rows of tiles, by waves that share the columns, each with a range of steps of its own.  Nothing is
-// shared before the end, where the sums of the waves are added in their order: X comes from the L2 into registers, AHEAD_X steps ahead, W AHEAD_W.
-// CH: steps of 32 columns between applications of a scale (1, 2, or 4)
 __device__ __forceinline__ float sum_over_halves(float x)             // of lanes n and 32 + n, in both
 {
     const auto b = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
@@ -329,10 +326,15 @@ __device__ __forceinline__ void store_sums(const MmParams &p, const RowTile &rt,
     }
 }
 
-template <int DT, int CH, bool ZEROS, int MT, int NT, int AHEAD_W, int AHEAD_X, int THREADS>
+// ---- up to 16 rows of X: a workgroup has them all and NT rows of tiles; its waves share the columns, each with a range of steps of its own, and nothing else
+// before the end, where their sums are added in their order.  X comes from the L2 straight into registers, AHEAD_X steps ahead, W AHEAD_W.  CH: chunks of 32
+// columns between applications of a scale (1, 2, or 4).
+// Bound by the reading of W: 64 pairs that meet 40 of 64 matrices of 2816 x 2048 in groups of 64 take 25.8 us, 5.0 TB/s, which is what a large copy reaches.
+// One row times 4096 x 4096 takes 4.5 us on the GPU, of which 3.4 are what any launch takes.
+template <int DT, int CH, bool ZEROS, int NT, int AHEAD_W, int AHEAD_X, int THREADS>
 __global__ void __launch_bounds__(THREADS) q4_split_kernel(const MmParams p)
 {
-    constexpr int kGroups = 4 / CH, kRows = 16 * MT;
+    constexpr int kGroups = 4 / CH, kRows = 16;
     extern __shared__ __attribute__((aligned(16))) float sums[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n_waves = 1 << p.lg_waves, n = lane & 15, q = lane >> 4;
     const uint32_t tile = p.by_col_blocks(blockIdx.x), col_block = blockIdx.x - tile * p.col_blocks;
@@ -349,7 +351,7 @@ __global__ void __launch_bounds__(THREADS) q4_split_kernel(const MmParams p)
 
     uint4v w[AHEAD_W][NT];
     Words<kGroups> sz[AHEAD_W][NT];
-    short8v xf[AHEAD_X][MT][4];
+    short8v xf[AHEAD_X][4];
     auto fetch_w = [&](auto d, int h, int t) {
         const uint32_t hh = h < further ? h : further;
         w[d][h] = *reinterpret_cast<const uint4v *>(w_at + ((hh * (uint32_t)n_tiles + (uint32_t)t) * 1024u + (uint32_t)lane * 16u));
@@ -363,37 +365,29 @@ __global__ void __launch_bounds__(THREADS) q4_split_kernel(const MmParams p)
     });
     // Rows behind the last one are out of X's range: loads of them cost nothing.
     const __amdgpu_buffer_rsrc_t x_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(p.X), 0, (int)p.x_bytes, 0x00020000);
-    uint32_t x_at[MT];
-#pragma unroll
-    for (int m = 0; m < MT; ++m)
-        x_at[m] = 16 * m + n < rt.count ? (uint32_t)x_row(p, y_row(p, rt.first + 16 * m + n)) * p.ldx_bytes + 16 * q : 0xFFFFF000u;
+    const uint32_t x_at = n < rt.count ? (uint32_t)x_row(p, y_row(p, rt.first + n)) * p.ldx_bytes + 16 * q : 0xFFFFF000u;
     auto fetch_x = [&](auto d, int t) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int chunk = 4 * t + i < p.k_chunks ? 4 * t + i : p.k_chunks - 1;
-#pragma unroll
-            for (int m = 0; m < MT; ++m) xf[d][m][i] = __builtin_bit_cast(short8v, __builtin_amdgcn_raw_buffer_load_b128(x_rsrc, (int)x_at[m], 64 * chunk, 0));
+            xf[d][i] = __builtin_bit_cast(short8v, __builtin_amdgcn_raw_buffer_load_b128(x_rsrc, (int)x_at, 64 * chunk, 0));
         }
     };
     static_for<AHEAD_X>([&](auto d) { fetch_x(d, tile_of(d)); });
 
-    float4v acc[MT][NT];
-    float taken[NT], of_x[MT];                                         // -s (16 + z) and the sum of x of the q-th of four groups
+    float4v acc[NT];
+    float taken[NT], of_x = 0.f;                                       // -s (16 + z) and the sum of x of the q-th of four groups
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int h = 0; h < NT; ++h) acc[m][h] = float4v{0, 0, 0, 0};
-#pragma unroll
-    for (int h = 0; h < NT; ++h) taken[h] = 0.f;
-#pragma unroll
-    for (int m = 0; m < MT; ++m) of_x[m] = 0.f;
+    for (int h = 0; h < NT; ++h) {
+        acc[h] = float4v{0, 0, 0, 0};
+        taken[h] = 0.f;
+    }
     auto take = [&]() {
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-            for (int h = 0; h < NT; ++h) acc[m][h] = __builtin_amdgcn_mfma_f32_16x16x4f32(of_x[m], taken[h], acc[m][h], 0, 0, 0);
-#pragma unroll
-        for (int h = 0; h < NT; ++h) taken[h] = 0.f;
+        for (int h = 0; h < NT; ++h) {
+            acc[h] = __builtin_amdgcn_mfma_f32_16x16x4f32(of_x, taken[h], acc[h], 0, 0, 0);
+            taken[h] = 0.f;
+        }
     };
     auto step = [&](auto d, auto more_w, auto more_x, int u) {
         constexpr int dx = d.value % AHEAD_X;
@@ -401,32 +395,23 @@ __global__ void __launch_bounds__(THREADS) q4_split_kernel(const MmParams p)
         if (4 * t + 4 > p.k_chunks) {                              // the last columns are fewer
 #pragma unroll
             for (int i = 1; i < 4; ++i)
-                if (4 * t + i >= p.k_chunks) {
-#pragma unroll
-                    for (int m = 0; m < MT; ++m) xf[dx][m][i] = short8v{0, 0, 0, 0, 0, 0, 0, 0};
-                }
+                if (4 * t + i >= p.k_chunks) xf[dx][i] = short8v{0, 0, 0, 0, 0, 0, 0, 0};
         }
 #pragma unroll
         for (int g = 0; g < kGroups; ++g) {
             const int slot = ((AHEAD_W % 4 == 0 ? d.value : u) * kGroups + g) & 3;
+            float sum = 0.f;
 #pragma unroll
-            for (int m = 0; m < MT; ++m) {
-                float s = 0.f;
-#pragma unroll
-                for (int i = g * CH; i < (g + 1) * CH; ++i) s += sum_of_8<DT>(__builtin_bit_cast(uint4v, xf[dx][m][i]));
-                s = sum_over_quarters(s);
-                of_x[m] = q == slot ? s : of_x[m];
-            }
+            for (int i = g * CH; i < (g + 1) * CH; ++i) sum += sum_of_8<DT>(__builtin_bit_cast(uint4v, xf[dx][i]));
+            sum = sum_over_quarters(sum);
+            of_x = q == slot ? sum : of_x;
 #pragma unroll
             for (int h = 0; h < NT; ++h) {
-                float4v part[MT];
-#pragma unroll
-                for (int m = 0; m < MT; ++m) part[m] = float4v{0, 0, 0, 0};
+                float4v part = float4v{0, 0, 0, 0};
 #pragma unroll
                 for (int i = g * CH; i < (g + 1) * CH; ++i) {
                     const short8v b = sixteen_plus(w[d][h][i]);
-#pragma unroll
-                    for (int m = 0; m < MT; ++m) part[m] = mfma16x16x32<DT>(xf[dx][m][i], b, part[m]);
+                    part = mfma16x16x32<DT>(xf[dx][i], b, part);
                 }
                 const float s = sz[d][h].template scale<DT>(g);
                 if constexpr (CH == 1) {
@@ -436,12 +421,9 @@ __global__ void __launch_bounds__(THREADS) q4_split_kernel(const MmParams p)
                 }
                 if (more_w.value && g == kGroups - 1) fetch_w(d, h, tile_of(u + AHEAD_W));
 #pragma unroll
-                for (int m = 0; m < MT; ++m)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[m][h][i] = __builtin_fmaf(s, part[m][i], acc[m][h][i]);
+                for (int i = 0; i < 4; ++i) acc[h][i] = __builtin_fmaf(s, part[i], acc[h][i]);
             }
             if (g == kGroups - 1 && slot == 3) take();
-            if constexpr (MT > 1) __builtin_amdgcn_sched_barrier(0);
         }
         if constexpr (more_x.value) fetch_x(constant<dx>(), tile_of(u + AHEAD_X));
     };
@@ -455,11 +437,9 @@ __global__ void __launch_bounds__(THREADS) q4_split_kernel(const MmParams p)
     if constexpr (CH > 1) take();                                      // what is left of four groups; of the others taken is zero
     float *mine = sums + (int64_t)wave * NT * kRows * kSumRow;
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
+    for (int h = 0; h < NT; ++h)
 #pragma unroll
-        for (int h = 0; h < NT; ++h)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) mine[(h * kRows + 16 * m + 4 * q + i) * kSumRow + n] = acc[m][h][i];
+        for (int i = 0; i < 4; ++i) mine[(h * kRows + 4 * q + i) * kSumRow + n] = acc[h][i];
     __syncthreads();
     store_sums<DT, NT, kRows>(p, rt, r0, sums, n_waves);
 }
@@ -577,7 +557,8 @@ __device__ __forceinline__ void store_32(const MmParams &p, int count, int token
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 }
 
-// Few workgroups: the division of the work as above, with X through a part of LDS that each wave has for itself.  A wave's load takes 256 bytes of four rows
+// Few workgroups: the division of the work as above (192 rows times 4096 x 14336 in groups of 128: 38.7 us, 583 TFLOP/s; the waits for X and the unpacking, which
+// is done once for each 64 rows, stand between it and the 883 of the kernel below), with X through a part of LDS that each wave has for itself.  A wave's load takes 256 bytes of four rows
 // (the pieces of 32 bytes that the matrix units take are a part of a line each, and the rest is gone from the L1 before it is asked for).  The rows of a
 // step are read into registers at once and those of the next step fetched into their place.
 template <int DT, int CH, bool ZEROS, int MT>
@@ -705,6 +686,9 @@ __global__ void __launch_bounds__(512) q4_mid_kernel(const MmParams p)
 
 // Many workgroups: 32 MT rows of X times 16 rows of tiles, by four waves with four rows of tiles each.  X goes through LDS, which all waves read; W
 // comes straight into registers, as it was laid out, and is turned into numbers there.
+// Bound by the issue of instructions: beside each product of 32 x 32 x 16, which takes the place of about six vector instructions, stand for 64 rows 2.5 that make
+// numbers of W, 2 that apply a scale (groups of 128) and the loads from LDS.  2048 rows times 8192 x 8192 reach 883 TFLOP/s with zero points and 967
+// without; a product of bf16 with bf16 of the library reaches 1186 at 8192 x 8192 x 8192.
 template <int CTRL>
 __device__ __forceinline__ float add_lane(float x)
 {
@@ -793,7 +777,7 @@ struct Variant {
 template <int DT, int CH, bool ZEROS, int NT, int AHEAD_W, int AHEAD_X, int THREADS>
 Variant split_variant(int waves)
 {
-    return {q4_split_kernel<DT, CH, ZEROS, 1, NT, AHEAD_W, AHEAD_X, THREADS>, 16, NT, 64 * waves, waves * NT * 16 * kSumRow * 4};
+    return {q4_split_kernel<DT, CH, ZEROS, NT, AHEAD_W, AHEAD_X, THREADS>, 16, NT, 64 * waves, waves * NT * 16 * kSumRow * 4};
 }
 template <int DT, int CH, bool ZEROS, int MT>
 Variant mid_variant(int waves)
@@ -871,8 +855,11 @@ MmParams mm_params(const q4_t *h, const void *X_dev, int64_t ldx, int64_t x_rows
 }
 
 // By how many workgroups there would be for the 256 compute units, in us (bf16, groups of 128, T rows times K x N):
-//   more than 16 rows: the kernel for many workgroups from 224 of them on (T 512, 4096 x 8192, 256 workgroups: 49, the other 55; T 192, 4096 x 14336, 168: 50 and
-//   46; T 256, 4096 x 8192, 128: 48 and 32); the other one with eight waves where a CU has one workgroup and each wave two steps (T 64, 8192 x 16384, 256
+//   more than 16 rows: the kernel for many workgroups from 256 of them on (T 512, 8192 x 8192, 256 workgroups: 98, the other 110; T 256, 4096 x 14336, 224: 53 and
+//   51; T 256, 8192 x 8192, 128: 93 and 53).  Of a plan's tiles some are filled in part only, and which is not known here: taken to be one for every two
+//   matrices beside the full ones, and 384 workgroups of them (16 experts of 4096 x 4096 with 64 rows each, 384: 78 and 80; with 48, 320: 74 and 68;
+//   32 of 4096 x 1536 with 32, 288: 51 and 39; 64 of 1408 x 2048 with 14, 480: 26 and 30), or 224 where a wave of the other one has a single step
+//   (128 of 512 x 512 with 48, 320: 16 and 22; with 14, 240: 9.5 and 12.5).  The other one with eight waves where a CU has one workgroup and each wave two steps (T 64, 8192 x 16384, 256
 //   workgroups: 34, with four 42; T 256, 4096 x 8192, 512: 39 and 32; T 57, 704 x 12878: 10.7 and 10.0)
 //   up to 16 rows: one row of tiles a workgroup and W four steps ahead while that is one workgroup for each CU (T 1, 4096 x 4096: 5.2, two rows 6.1; T 1,
 //   8192 x 8192: 11.1 and 9.7).  Else two, and nothing ahead but the next step: then eight waves of a SIMD hide each other's waits (W four steps ahead
@@ -881,11 +868,12 @@ MmParams mm_params(const q4_t *h, const void *X_dev, int64_t ldx, int64_t x_rows
 //   8192 x 8192, 512 rows of tiles: 14.6 and 12.0).
 //   Eight waves where each has two steps or workgroups are few (T 1, 2048 x 14336: 6.3, four 6.4; T 8, 8192 x 8192: 9.9 and 13.2; 8 pairs, 2048 x 1536: 7.0 and
 //   7.4), four where there are many (64 pairs of 64 experts, 2048 x 2816: 24.8, eight 25.5; 1408 x 2048: 14.9 and 16.2)
-Choice choose(const MmParams &p, int32_t rows, int64_t row_tiles, int64_t rows_each)
+Choice choose(const MmParams &p, int32_t rows, int64_t row_tiles, int64_t rows_each, int64_t n_mats)
 {
     const int64_t tiles = row_tiles * p.tile_rows;
     if (rows > 16) {
-        if (row_tiles * ((p.tile_rows + 15) / 16) >= 224) return {rows, 16, 4};
+        const int64_t filled = p.order ? std::min(row_tiles, p.n_rows / rows + n_mats / 2) : row_tiles;
+        if (filled * ((p.tile_rows + 15) / 16) >= (p.order ? p.k_tiles <= 4 ? 224 : 384 : 256)) return {rows, 16, 4};
         return {rows, 4, row_tiles * ((p.tile_rows + 3) / 4) <= 256 && p.k_tiles >= 16 ? 8 : 4};
     }
     if (tiles <= 256 && !p.gated) return {16, 1, p.k_tiles >= 32 ? 8 : 4};
@@ -902,7 +890,7 @@ void set_y(MmParams &p, int32_t y_type)
 int launch_mm(const q4 *h, MmParams &p, int32_t rows, int64_t row_tiles, int64_t rows_each, void *hip_stream)
 {
     if (rows == 16 && p.x_bytes == 0) rows = 32;       // an X of 4 GiB and more: the other kernels have 64-bit addresses
-    const Choice c = choose(p, rows, row_tiles, rows_each);
+    const Choice c = choose(p, rows, row_tiles, rows_each, h->n_mats);
     const Variant v = h->dtype == VBR_F16 ? mm_variant<VBR_F16>(h->group, h->zeros, c) : mm_variant<VBR_BF16>(h->group, h->zeros, c);
     p.col_blocks = (int32_t)((p.tile_rows + v.tile_rows - 1) / v.tile_rows);
     p.by_col_blocks = Divide::by(p.col_blocks);

@@ -12,7 +12,8 @@ namespace vbrk {
 constexpr int32_t kMaxExperts = 1024;              // one thread of a workgroup each, in the scan
 constexpr int32_t kMaxTopK = 64, kMaxGroups = 64;  // one lane each
 constexpr int64_t kMaxPairs = 1 << 30;             // positions are 32 bits
-constexpr int64_t kPlanPart = 4096;                // pairs of a workgroup, at least, where there are several
+constexpr int64_t kPlanAlone = 4096;               // pairs up to which one workgroup groups them all
+constexpr int64_t kPlanPart = 1024;                // pairs of a workgroup, at least, where there are several
 
 constexpr int64_t kMostThreads = 0xFFFFFFFFll;     // of a launch
 

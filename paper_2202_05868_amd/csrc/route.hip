@@ -15,7 +15,7 @@ namespace vbrk {
 namespace {
 
 constexpr int kRouteThreads = 256;     // 4 waves
-constexpr int64_t kNarrowRows = 4096;  // rows from which on 16 lanes have one
+constexpr int64_t kNarrowRows = 2048;  // rows from which on 16 lanes have one
 
 template <int TY>
 __device__ __forceinline__ float load_as_f32(const void *p, int64_t i)
@@ -33,7 +33,7 @@ __device__ __forceinline__ void store_f32(void *p, int64_t i, float v)          
     else static_cast<__bf16 *>(p)[i] = (__bf16)v;
 }
 
-// exp(x), x at most a little above 0, within three steps: 2^t (1 + r), r what rounding took from t = x log2(e); 0 for -inf
+// exp(x), x at most a little above 0, within three steps: 2^t (1 + r), r what rounding took from t = x log2(e); 0 for -inf and NaN
 __device__ __forceinline__ float exp_of(float x)
 {
     constexpr float log2e = 1.44269502f, rest = 1.92596299e-8f, ln2 = 0.693147181f;      // log2(e) in two numbers
@@ -74,17 +74,36 @@ template <int LP>
 __device__ __forceinline__ float row_sum(float x) { return number(over_lanes<LP>(bits(x), [](uint32_t a, uint32_t b) { return bits(number(a) + number(b)); })); }
 template <int LP>
 __device__ __forceinline__ int row_min(int x) { return (int)over_lanes<LP>((uint32_t)x, [](uint32_t a, uint32_t b) { return a < b ? a : b; }); }     // none is negative
-template <int LP>
-__device__ __forceinline__ double row_max(double x)
+// over the whole wave, in 64 bits
+template <int CTRL>
+__device__ __forceinline__ double from_lane(double x)
 {
-    for (int m = LP / 2; m; m >>= 1) x = fmax(x, __shfl_xor(x, m));
+    const uint64_t b = __builtin_bit_cast(uint64_t, x);
+    return __builtin_bit_cast(double, (uint64_t)from_lane<CTRL>((uint32_t)(b >> 32)) << 32 | from_lane<CTRL>((uint32_t)b));
+}
+__device__ __forceinline__ double wave_max(double x)
+{
+    x = fmax(x, from_lane<0xB1>(x));
+    x = fmax(x, from_lane<0x4E>(x));
+    x = fmax(x, from_lane<0x141>(x));
+    x = fmax(x, from_lane<0x140>(x));
+    auto swap = [&](auto f) {
+        const uint64_t b = __builtin_bit_cast(uint64_t, x);
+        const auto hi = f((uint32_t)(b >> 32)), lo = f((uint32_t)b);
+        return fmax(__builtin_bit_cast(double, (uint64_t)(uint32_t)hi[0] << 32 | (uint32_t)lo[0]), __builtin_bit_cast(double, (uint64_t)(uint32_t)hi[1] << 32 | (uint32_t)lo[1]));
+    };
+    x = swap([](uint32_t h) { return __builtin_amdgcn_permlane16_swap(h, h, false, false); });
+    return swap([](uint32_t h) { return __builtin_amdgcn_permlane32_swap(h, h, false, false); });
+}
+__device__ __forceinline__ double wave_sum(double x)
+{
+    for (int m = 32; m; m >>= 1) x += __shfl_xor(x, m);
     return x;
 }
-template <int LP>
-__device__ __forceinline__ double row_sum(double x)
+__device__ __forceinline__ double of_lane(double x, int lane)
 {
-    for (int m = LP / 2; m; m >>= 1) x += __shfl_xor(x, m);
-    return x;
+    const uint64_t b = __builtin_bit_cast(uint64_t, x);
+    return __builtin_bit_cast(double, (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(b >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)b, lane));
 }
 
 // V consecutive experts of a row, the first of them e0; those that are not there are closed
@@ -129,58 +148,6 @@ struct TopkParams {
     float scale;
 };
 
-// The choice among the keys, V a lane, in 64 bits: lane j of the row gets the j-th expert, -1 without one.  Of equal keys the lower index wins.
-template <int LP, int V>
-__device__ __forceinline__ int choose_exactly(const TopkParams &p, double (&key)[V], const float (&l)[V], double *lds, int sub)
-{
-    if (p.n_groups > p.top_groups) {
-        // keys by way of LDS (one more place after every 16, or lanes meet in the same bank), a group a lane
-#pragma unroll
-        for (int v = 0; v < V; ++v) lds[(sub * V + v) + ((sub * V + v) >> 4)] = key[v];
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        double best = -INFINITY, second = -INFINITY;
-        if (sub < p.n_groups) {
-            for (int i = 0; i < p.group_size; ++i) {
-                const int e = sub * p.group_size + i;
-                const double x = lds[e + (e >> 4)];
-                second = x > best ? best : x > second ? x : second;
-                best = x > best ? x : best;
-            }
-        }
-        double mine = second > -INFINITY ? best + second : best;
-        uint64_t chosen = 0;
-        for (int i = 0; i < p.top_groups; ++i) {
-            const double top = row_max<LP>(mine);
-            const int at = row_min<LP>(mine == top && top > -INFINITY ? sub : INT_MAX);
-            if (at != INT_MAX) chosen |= 1ull << at;
-            if (sub == at) mine = -INFINITY;
-        }
-#pragma unroll
-        for (int v = 0; v < V; ++v)
-            if (sub * V + v < p.n_experts && !(chosen >> ((uint32_t)(sub * V + v) * p.group_factor >> 20) & 1)) key[v] = -INFINITY;
-    }
-    if (p.bias == nullptr) {                              // the same order, and exact
-#pragma unroll
-        for (int v = 0; v < V; ++v) key[v] = key[v] > -INFINITY ? (double)l[v] : (double)-INFINITY;
-    }
-    int my_id = -1;
-    for (int j = 0; j < p.top_k; ++j) {
-        double top = key[0];
-#pragma unroll
-        for (int v = 1; v < V; ++v) top = key[v] > top ? key[v] : top;
-        int mine = 0;
-#pragma unroll
-        for (int v = V - 1; v >= 0; --v) mine = key[v] == top ? v : mine;
-        const double most = row_max<LP>(top);
-        const int at = row_min<LP>(top == most && most > -INFINITY ? sub * V + mine : INT_MAX);
-        if (sub == j) my_id = at == INT_MAX ? -1 : at;
-        const int taken = at - sub * V;
-#pragma unroll
-        for (int v = 0; v < V; ++v) key[v] = taken == v ? -INFINITY : key[v];
-    }
-    return my_id;
-}
-
 // Numbers as integers of the same order
 __device__ __forceinline__ int ordered(float x)
 {
@@ -191,6 +158,104 @@ __device__ __forceinline__ float of_ordered(int i) { return number((uint32_t)(i 
 
 template <int LP>
 __device__ __forceinline__ int row_max_int(int x) { return (int)over_lanes<LP>((uint32_t)x, [](uint32_t a, uint32_t b) { return (uint32_t)((int)a > (int)b ? (int)a : (int)b); }); }
+constexpr int kClosed = (int)0x807FFFFF, kLargest = 0x7F7FFFFF;      // of -inf, and no number is as low; of FLT_MAX
+
+// The choice among the keys, V a lane of the wave, in 64 bits: lane j gets the j-th expert, -1 without one.  Of equal keys the lower index wins.
+template <int V>
+__device__ __forceinline__ int choose_exactly(const TopkParams &p, double (&key)[V], const float (&l)[V], double *lds, int sub)
+{
+    if (p.n_groups > p.top_groups) {
+        double best = -INFINITY, second = -INFINITY;
+        const int lanes = p.group_size / V;                // of a group, if a group is whole lanes, 1, 2, 4, 8 or 16 of them
+        const bool by_lanes = lanes * V == p.group_size && lanes <= 16 && (lanes & (lanes - 1)) == 0;
+        if (by_lanes) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                second = fmax(fmin(key[v], best), second);
+                best = fmax(best, key[v]);
+            }
+            auto merge = [&](double b, double s) {
+                second = fmax(fmin(best, b), fmax(second, s));
+                best = fmax(best, b);
+            };
+            if (lanes >= 2) merge(from_lane<0xB1>(best), from_lane<0xB1>(second));
+            if (lanes >= 4) merge(from_lane<0x4E>(best), from_lane<0x4E>(second));
+            if (lanes >= 8) merge(from_lane<0x141>(best), from_lane<0x141>(second));
+            if (lanes >= 16) merge(from_lane<0x140>(best), from_lane<0x140>(second));
+        } else {
+            // keys by way of LDS (one more place after every 16, or lanes meet in the same bank), a group a lane
+#pragma unroll
+            for (int v = 0; v < V; ++v) lds[(sub * V + v) + ((sub * V + v) >> 4)] = key[v];
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            if (sub < p.n_groups) {
+#pragma unroll 4
+                for (int i = 0; i < p.group_size; ++i) {
+                    const int e = sub * p.group_size + i;
+                    const double x = lds[e + (e >> 4)];
+                    second = fmax(fmin(x, best), second);
+                    best = fmax(best, x);
+                }
+            }
+        }
+        const double mine = second > -INFINITY ? best + second : best;
+        const int step = by_lanes ? lanes : 1;             // from a group's first lane to the next one's
+        int ahead = 0;                                     // groups that come before this lane's
+        for (int g = 0; g < p.n_groups; ++g) {
+            const double other = of_lane(mine, g * step);
+            ahead += (other > mine) | ((other == mine) & (g * step + step <= sub));
+        }
+        const bool stays = ahead < p.top_groups && mine > -INFINITY;
+        if (by_lanes) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) key[v] = stays ? key[v] : -INFINITY;
+        } else {
+            const uint64_t chosen = __ballot(stays);
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+                if (sub * V + v < p.n_experts && !(chosen >> ((uint32_t)(sub * V + v) * p.group_factor >> 20) & 1)) key[v] = -INFINITY;
+        }
+    }
+    // Rounded to 32 bits they keep their order, but for those that become equal: only these are compared in 64.
+    int x[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        if (p.bias == nullptr && key[v] > -INFINITY) key[v] = l[v];      // the same order, and exact
+        x[v] = ordered((float)key[v]);
+    }
+    int my_id = -1;
+    for (int j = 0; j < p.top_k; ++j) {
+        int first = x[0];
+#pragma unroll
+        for (int v = 1; v < V; ++v) first = max(first, x[v]);
+        const int most = row_max_int<64>(first);
+        if (most <= kClosed) break;
+        int n = 0, mine = 0;
+        uint64_t lanes = 0;
+#pragma unroll
+        for (int v = V - 1; v >= 0; --v) {
+            const uint64_t have = __ballot(x[v] == most);
+            n += __popcll(have);
+            lanes |= have;
+            mine = x[v] == most ? v : mine;
+        }
+        int at = __builtin_amdgcn_readlane(sub * V + mine, __builtin_ctzll(lanes));
+        if (n > 1) {
+            double top = -INFINITY;
+#pragma unroll
+            for (int v = V - 1; v >= 0; --v) {
+                const bool as_high = x[v] == most && key[v] >= top;
+                top = as_high ? key[v] : top;
+                mine = as_high ? v : mine;
+            }
+            const double highest = wave_max(top);
+            at = row_min<64>(first == most && top == highest ? sub * V + mine : INT_MAX);
+        }
+        if (sub == j) my_id = at;
+#pragma unroll
+        for (int v = 0; v < V; ++v) x[v] = at == sub * V + v ? kClosed : x[v];
+    }
+    return my_id;
+}
 
 // falling, by merging odd and even places: comparators that are known beforehand
 template <int V>
@@ -211,20 +276,21 @@ __device__ __forceinline__ void sort_falling(int (&x)[V])
                     }
 }
 
-constexpr int kClosed = INT_MIN;
-
 // The same in 32 bits.  Keys are whole numbers in the order of the numbers, with an expert's place in its lane in the lowest bits, lower places first: a lane sorts
-// its keys once, and a choice is the largest of the lanes' first ones.  `bound` is what the difference of two keys may be off by, before the lowest bits
-// are lost; the result says whether any difference that decides may be of the other sign.  exact: neither is; then there is nothing to say.
+// its keys once, and a choice is the largest of the lanes' first ones.  The result says whether any difference that decides may be of the other sign.  `bound`
+// is what the difference of two keys may be off by, and a key without its lowest bits is lower by up to V steps: of two that differ the higher one is
+// higher by at least the difference less V steps of the lower.  Raw scores are what they are: those that differ without their lowest bits are in order.
+// widest: the largest of the row's finite keys in magnitude.  exact: the lowest bits were zero, and there is nothing to say.
 template <int LP, int V>
-__device__ __forceinline__ bool choose(const TopkParams &p, const float (&key)[V], const float (&l)[V], float *lds, int sub, int &my_id, float bound, bool exact)
+__device__ __forceinline__ bool choose(const TopkParams &p, const float (&key)[V], const float (&l)[V], float *lds, int sub, int &my_id, float bound, float widest, bool exact)
 {
     bool unsure = false;              // (the same in every lane of the row)
-    uint64_t chosen = ~0ull;
+    uint64_t chosen = ~0ull;          // groups
+    bool stays = true;                // by lanes: this lane's is
     int x[V];
     auto pack = [&](const float (&from)[V]) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) x[v] = key[v] > -INFINITY ? (ordered(fminf(from[v], FLT_MAX)) & -V) | (V - 1 - v) : kClosed;
+        for (int v = 0; v < V; ++v) x[v] = (min(ordered(from[v]), kLargest) & -V) | (V - 1 - v);
     };
     const bool by_raw = p.bias == nullptr;                // the same order, and exact
     const bool by_lanes = p.lanes_a_group && !by_raw;
@@ -233,7 +299,7 @@ __device__ __forceinline__ bool choose(const TopkParams &p, const float (&key)[V
         sort_falling(x);
     }
     if (p.n_groups > p.top_groups) {
-        float mine, before = INFINITY, wide = bound;
+        float mine, before = INFINITY, wide = 2 * bound + widest * 0x1p-22f;      // of the sums of two keys, which are rounded
         int group = sub;
         if (by_lanes) {
             int best = x[0], second = V > 1 ? x[V > 1] : kClosed;
@@ -244,7 +310,8 @@ __device__ __forceinline__ bool choose(const TopkParams &p, const float (&key)[V
             if (p.lanes_a_group >= 2) merge((int)from_lane<0xB1>((uint32_t)best), (int)from_lane<0xB1>((uint32_t)second));
             if (p.lanes_a_group >= 4) merge((int)from_lane<0x4E>((uint32_t)best), (int)from_lane<0x4E>((uint32_t)second));
             if (p.lanes_a_group >= 8) merge((int)from_lane<0x141>((uint32_t)best), (int)from_lane<0x141>((uint32_t)second));
-            mine = best == kClosed ? -INFINITY : of_ordered(best) + (second == kClosed ? 0.f : of_ordered(second));
+            mine = best <= kClosed ? -INFINITY : of_ordered(best & -V) + (second <= kClosed ? 0.f : of_ordered(second & -V));
+            wide += widest * (2 * V * 0x1p-23f);
             group = sub / p.lanes_a_group;
         } else {
             // by way of LDS (one more place after every 16, or lanes meet in the same bank), a group a lane
@@ -263,14 +330,27 @@ __device__ __forceinline__ bool choose(const TopkParams &p, const float (&key)[V
             }
             mine = second > -INFINITY ? best + second : best;
         }
-        chosen = 0;
-        for (int i = 0; i <= p.top_groups; ++i) {
-            const float top = row_max<LP>(mine);
-            const int at = row_min<LP>(mine == top && top > -INFINITY ? group : INT_MAX);
-            if (i == p.top_groups) unsure = top > -INFINITY && before - top <= 2 * wide + (fabsf(before) + fabsf(top)) * (V * 0x1p-22f);      // two keys each
-            else if (at != INT_MAX) chosen |= 1ull << at;
-            if (group == at) mine = -INFINITY;
-            before = top;
+        if constexpr (LP == 16) {
+            // By how many are before it; of equal ones that would be chosen together too many are, and the row is in doubt.
+            int ahead = 0;
+            static_for<15>([&](auto i) { ahead += number(from_lane<0x121 + i.value>(bits(mine))) > mine; });      // the other lanes, turned in the row
+            const int wanted = p.top_groups * (by_lanes ? p.lanes_a_group : 1);
+            stays = ahead < wanted && mine > -INFINITY;
+            const uint32_t in = (uint32_t)(__ballot(stays) >> (threadIdx.x & 48)) & 0xFFFFu;
+            const float last = -row_max<LP>(stays ? -mine : -INFINITY), next = row_max<LP>(stays ? -INFINITY : mine);
+            unsure = __popc(in) > wanted || (next > -INFINITY && last - next <= wide);
+            chosen = in;
+        } else {
+            chosen = 0;
+            for (int i = 0; i <= p.top_groups; ++i) {
+                const float top = row_max<LP>(mine);
+                const int at = row_min<LP>(mine == top && top > -INFINITY ? group : INT_MAX);
+                if (i == p.top_groups) unsure = top > -INFINITY && before - top <= wide;
+                else if (at != INT_MAX) chosen |= 1ull << at;
+                if (group == at) mine = -INFINITY;
+                before = top;
+            }
+            stays = chosen >> group & 1;
         }
     }
     if (by_raw) {
@@ -280,19 +360,22 @@ __device__ __forceinline__ bool choose(const TopkParams &p, const float (&key)[V
             for (int v = 0; v < V; ++v) x[v] = chosen >> ((uint32_t)(sub * V + v) * p.group_factor >> 20) & 1 ? x[v] : kClosed;
         }
         sort_falling(x);
+    } else if (by_lanes) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) x[v] = stays ? x[v] : kClosed;
     } else if (p.n_groups > p.top_groups) {
 #pragma unroll
         for (int v = 0; v < V; ++v) x[v] = chosen >> ((uint32_t)(sub * V + V - 1 - (x[v] & (V - 1))) * p.group_factor >> 20) & 1 ? x[v] : kClosed;
-        if (!by_lanes) sort_falling(x);                   // (by lanes, a lane has all or none)
+        sort_falling(x);
     }
-    const float by = by_raw ? 0.f : bound;
+    const float by = by_raw ? 0.f : bound, lost = by_raw ? 0.f : V * 0x1p-23f;
     float before = INFINITY;
     for (int j = 0; j < p.top_k + (exact ? 0 : 1); ++j) {
         const int first = x[0] & -V, most = row_max_int<LP>(first), mine = sub * V + V - 1 - (x[0] & (V - 1));      // (places count among equal keys only)
-        const int at = row_min<LP>(first == most && most != kClosed ? mine : INT_MAX);
+        const int at = row_min<LP>(first == most && most > kClosed ? mine : INT_MAX);
         if (!exact) {
             const float now = of_ordered(most);
-            unsure |= j > 0 && most != kClosed && before - now <= by + (fabsf(before) + fabsf(now)) * (V * 0x1p-23f);
+            unsure |= j > 0 && most > kClosed && before - now <= by + fabsf(now) * lost;
             before = now;
         }
         if (j < p.top_k && sub == j) my_id = at == INT_MAX ? -1 : at;
@@ -327,7 +410,7 @@ __device__ __forceinline__ int choose_row_exactly(const TopkParams &p, int64_t r
             key[v] = exp(p.sigmoid ? -x : x - most);
             total += l[v] > -INFINITY ? key[v] : 0.0;
         }
-        if (!p.sigmoid) total = row_sum<64>(total);
+        if (!p.sigmoid) total = wave_sum(total);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             key[v] = (p.sigmoid ? 1.0 / (1.0 + key[v]) : key[v] / total) + (double)bias[v];
@@ -337,11 +420,13 @@ __device__ __forceinline__ int choose_row_exactly(const TopkParams &p, int64_t r
 #pragma unroll
         for (int v = 0; v < V; ++v) key[v] = l[v];
     }
-    return choose_exactly<64, V>(p, key, l, lds, lane);
+    return choose_exactly<V>(p, key, l, lds, lane);
 }
 
 // LP lanes a row, V experts a lane.  What decides between sums of scores and biases are differences that 32 bits may not tell: they are made in 32 bits, with a
 // bound for what they are off by, and where a difference is within it, in 64 bits.  Raw scores are compared as they are: the score rises with them.
+// Bound by the issue of vector instructions, some 1700 for four rows of 256 experts, most of them the sorting of a lane's keys and the choice itself: 16384 rows, 8
+// of 256 in 4 of 8 groups take 16 us, of which the rows in doubt are about 4; 8192 rows, 8 of 128 by raw scores 4.6.
 template <int TY, int LP, int V>
 __global__ void __launch_bounds__(kRouteThreads) route_topk_kernel(const TopkParams p)
 {
@@ -365,7 +450,7 @@ __global__ void __launch_bounds__(kRouteThreads) route_topk_kernel(const TopkPar
         top = row_max<LP>(top);
         total = 0.f;
 #pragma unroll
-        for (int v = 0; v < V; ++v) total += l[v] > -INFINITY ? exp_of(l[v] - top) : 0.f;
+        for (int v = 0; v < V; ++v) total += exp_of(l[v] - top);                 // (0 of one that is closed)
         total = row_sum<LP>(total);
     }
     int my_id = -1;
@@ -380,19 +465,26 @@ __global__ void __launch_bounds__(kRouteThreads) route_topk_kernel(const TopkPar
         }
         float widest = 0.f;
         const float one_of_total = 1.f / total;
+        if (p.sigmoid) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) key[v] = sigmoid_of(l[v]);
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v) key[v] = exp_of(l[v] - top) * one_of_total;
+        }
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const float s = (p.sigmoid ? sigmoid_of(l[v]) : exp_of(l[v] - top) * one_of_total) + bias[v];
-            key[v] = l[v] > -INFINITY && s > -INFINITY ? s : -INFINITY;
-            widest = fmaxf(widest, fabsf(key[v]) < INFINITY ? fabsf(key[v]) : 0.f);
+            const float s = l[v] > -INFINITY ? key[v] + bias[v] : -INFINITY;
+            key[v] = s > -INFINITY ? s : -INFINITY;                        // (NaN closes)
+            widest = fmaxf(widest, fabsf(s) < INFINITY ? fabsf(s) : 0.f);
         }
         widest = row_max<LP>(widest);
-        // A sigmoid is off by 8 half steps at 1 at most (exponential, sum, reciprocal, product), a softmax by those and what V + 6 additions in a row
-        // leave in its sum, and the sum with the bias by half a step of itself; two of them differ by as much again.
-        unsure = choose<LP, V>(p, key, l, row_lds, sub, my_id, 0x1p-24f * (2 * (p.sigmoid ? 8 : 18 + V) + 4 * widest), false);
+        // A sigmoid is off by 8 half steps at 1 at most (exponential, sum, reciprocal, product), a softmax by those of the largest one, 1 / total, and what
+        // V + 6 additions in a row leave in its sum, and the sum with the bias by half a step of itself; two of them differ by as much again.
+        unsure = choose<LP, V>(p, key, l, row_lds, sub, my_id, 0x1p-24f * ((p.sigmoid ? 16.f : (36 + 2 * V) * one_of_total) + 4 * widest), widest, false);
     } else {
         // numbers of 16 bits leave the lowest bits of 32 free, and nothing is lost
-        unsure = choose<LP, V>(p, l, l, row_lds, sub, my_id, 0.f, TY != VBR_F32);
+        unsure = choose<LP, V>(p, l, l, row_lds, sub, my_id, 0.f, 0.f, TY != VBR_F32);
     }
     // rows in doubt, one after the other, by the whole wave
     for (uint64_t doubt = __ballot(unsure); doubt != 0;) {
@@ -438,7 +530,7 @@ struct TopkGradParams {
 //   renormalised   dl = scale r_j (dw_j - c), times (1 - s_j) for sigmoids, at the chosen experts, zero elsewhere
 //   sigmoid        dl = scale dw_j s_j (1 - s_j) at the chosen ones
 //   softmax        dl = scale p_e (dw_e - sum_j dw_j p_j) everywhere
-// Only the last one reads all raw scores.
+// Only the last one reads all raw scores.  Bound by what it writes and the launch: 8192 rows of 128 experts, choice and gradient, take 7.5 us.
 template <int TY, int LP, int V>
 __global__ void __launch_bounds__(kRouteThreads) route_topk_grad_kernel(const TopkGradParams p)
 {
@@ -461,7 +553,7 @@ __global__ void __launch_bounds__(kRouteThreads) route_topk_grad_kernel(const To
         top = row_max<LP>(top);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            l[v] = l[v] > -INFINITY ? exp_of(l[v] - top) : 0.f;
+            l[v] = exp_of(l[v] - top);                                         // (0 of one that is closed)
             total += l[v];
         }
         total = row_sum<LP>(total);
@@ -523,6 +615,7 @@ __global__ void __launch_bounds__(kRouteThreads) route_topk_grad_kernel(const To
 // ---- the grouping.  A workgroup owns consecutive pairs and each of its 16 waves a part of them, which it counts by expert in LDS.  With the counts of the
 // workgroups and waves before it a wave knows where its first pair of every expert belongs, goes over its pairs again and puts them there: pairs of an
 // expert stay in their order.  One workgroup needs no other's counts; of several, a first launch leaves them in the plan.
+// Bound by its launches and the trips to memory and LDS that follow each other: 128 pairs of 64 experts take 4.7 us, 131072 of 256 10.8.
 constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64;
 
 __device__ __forceinline__ uint64_t same_id(int id, int bits)      // lanes with this lane's id
@@ -748,8 +841,8 @@ __device__ __forceinline__ void store8(void *p, int64_t i, const float (&x)[8])
     }
 }
 
-// A thread owns eight columns of a row of out; the row's results are added in the order of their places.  Bound by what it reads; AT places are on
-// their way at a time (of one that does not count, the first one's, without effect).
+// A thread owns eight columns of a row of out; the row's results are added in the order of their places.  Bound by what it reads: 4096 rows of 8 bf16 results of
+// 2048 take 38 us, 4.0 TB/s.  AT places are on their way at a time (of one that does not count, the first one's, without effect).
 template <int TY, int TO, int AT>
 __global__ void __launch_bounds__(kRouteThreads) route_combine_kernel(const CombineParams p)
 {
@@ -779,7 +872,8 @@ __global__ void __launch_bounds__(kRouteThreads) route_combine_kernel(const Comb
     store8<TO>(p.out, row * p.ldo + col, sum);
 }
 
-// A wave owns a pair: dy = w dout, dw = dout . y.  The k waves of a row read its dout from the caches.
+// A wave owns a pair: dy = w dout, dw = dout . y.  The k waves of a row read its dout from the caches.  Bound by what it reads and writes: for the rows above
+// 49 us, 5.8 TB/s, part of it from the cache behind the L2.
 template <int TY, int TO>
 __global__ void __launch_bounds__(kRouteThreads) route_combine_grad_kernel(const CombineParams p)
 {
@@ -829,7 +923,9 @@ bool float_type(int32_t t) { return t == VBR_F16 || t == VBR_BF16 || t == VBR_F3
 bool aligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 int64_t up(int64_t x, int64_t q) { return (x + q - 1) / q * q; }
 
-// Lanes of a row: 16 where they can hold the experts and there are rows for every SIMD, four a wave, 64 elsewhere: one row of them is done sooner.
+// Lanes of a row: 16 where they can hold the experts and there are many rows, four a wave, 64 elsewhere: one row of them is done sooner.  In us with 16 and 64,
+// 8 of 256 experts in 8 groups: 1024 rows 9.5 and 6.0, 2048 9.8 and 9.4, 4096 9.9 and 12.9, 16384 17.1 and 27.8; 8 of 128: 512 5.5 and 5.9, 2048 4.2 and 4.6,
+// 16384 5.9 and 13.4; 4 of 64: 1024 3.7 and 3.6, 2048 3.7 and 3.7, 16384 4.5 and 8.5.
 struct Width {
     int32_t lanes, each;
 };
@@ -866,7 +962,10 @@ bool whole_pieces(const void *rows, int64_t ld, uintptr_t size) { return aligned
 
 }  // namespace
 
-// Rows of a tile of the products: by how many pairs an expert has if all have alike.
+// Rows of a tile of the products: by how many pairs an expert has if all have alike.  A tile reads its expert's matrix once, a larger one multiplies more rows
+// that are not there.  In us, with tiles of 16, 32 and 64 rows, for 64 experts of 2816 x 2048 and 2048 x 1408 with
+//   8 pairs each:  52 50 76 and 22 25 31     12:  55 50 76 and 29 25 32     16:  68 51 79 and 34 26 31
+//   32:  100 68 81 and 56 31 32              48:  133 89 80 and 75 41 34    64:  163 106 95 and 97 46 49
 int32_t plan_tile_rows(int64_t n_pairs, int32_t n_experts)
 {
     const int64_t rows = n_pairs / n_experts;
@@ -885,8 +984,9 @@ PlanParts plan_parts(int64_t n_pairs, int32_t n_experts)
     PlanParts q;
     q.tile_rows = plan_tile_rows(n_pairs, n_experts);
     q.n_tiles = plan_max_tiles(n_pairs, n_experts, q.tile_rows);
-    // workgroups of at least kPlanPart pairs, and no more than there are compute units
-    q.n_parts = std::max<int64_t>(1, std::min<int64_t>(256, n_pairs / kPlanPart));
+    // One workgroup needs one launch (4096 pairs of 64 experts 7.7 us, four workgroups 8.1; 8192 pairs 11.3, eight of them 8.0); of several each has at least kPlanPart
+    // pairs (32768 of 256 experts 9.2 us, with 2048 each 10.8), and there are no more than compute units.
+    q.n_parts = n_pairs <= kPlanAlone ? 1 : std::min<int64_t>(256, n_pairs / kPlanPart);
     q.per_wave = up((n_pairs + q.n_parts * kPlanWaves - 1) / (q.n_parts * kPlanWaves), 64);
     q.order = up(4 * ((int64_t)n_experts + 1), 256);
     q.tiles = up(q.order + 4 * n_pairs, 256);
@@ -1020,8 +1120,6 @@ int combine_args(int32_t y_type, int32_t out_type, int64_t n_cols, int64_t n_row
 template <int TY, int TO>
 constexpr auto route_combine_2 = route_combine_kernel<TY, TO, 2>;
 template <int TY, int TO>
-constexpr auto route_combine_4 = route_combine_kernel<TY, TO, 4>;
-template <int TY, int TO>
 constexpr auto route_combine_8 = route_combine_kernel<TY, TO, 8>;
 
 #define COMBINE_LAUNCH(KERNEL, TY, TO) hipLaunchKernelGGL((KERNEL<TY, TO>), dim3((unsigned)grid), dim3(kRouteThreads), 0, stream, p)
@@ -1064,8 +1162,9 @@ extern "C" int route_combine(const void *y_dev, int64_t ldy, int32_t y_type, con
     const int64_t grid = (n_rows * p.n_chunks + kRouteThreads - 1) / kRouteThreads;
     if (grid > kMostThreads / 2 / kRouteThreads) return VBR_EUNSUPPORTED;          // (threads are divided by n_chunks in 31 bits)
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    if (top_k <= 2) COMBINE_BY_TYPES(route_combine_2);
-    else if (top_k <= 4) COMBINE_BY_TYPES(route_combine_4);
+    // two places at a time, or eight where there are as many (in us; 16384 fp32 results of 2048 columns, 8 a row: 24.8, with two 26.4; 6 a row: 28.8 and 26.6;
+    // one a row: 85.8 and 46.7, since what is not there is read as well)
+    if (top_k < 8) COMBINE_BY_TYPES(route_combine_2);
     else COMBINE_BY_TYPES(route_combine_8);
     return launched();
 }
