@@ -132,7 +132,7 @@ struct MmParams {
     int64_t ldx, ldy, n_rows;                  // rows of Y
     int64_t k_tiles, tile_rows, steps;
     uint32_t x_bytes, ldx_bytes;               // of X from its first element to its last; of a row to the next; 0 where that is beyond 32 bits
-    int32_t half, k_chunks, lg_waves;          // k_chunks: columns / 32; lg_waves: of the waves of a workgroup that share the columns
+    int32_t half, k_chunks, lg_waves;          // k_chunks: columns / 32; lg_waves: of the waves of a workgroup that share the columns (of a pair)
     uint32_t step_divide;                      // tile t is of step t, or t step_divide >> 32 where that is not zero
     int32_t gated, f32, fours;                 // fours: four elements of Y from a multiple of four on are aligned to as much
     int32_t col_blocks;                        // of the launch: workgroup i has tile of rows i / col_blocks
@@ -142,6 +142,8 @@ struct MmParams {
     const int32_t *order;
     const int32_t *ids;                        // or, of pairs that each have a tile of their own, these and how many matrices there are
     int32_t n_mats;
+    const float *weights;                      // of the pairs, of a sum over top_k of them in bf16 or not
+    int32_t top_k, bf16;
     Divide by_places;                          // the pairs of a row of X
 };
 
@@ -251,14 +253,14 @@ __device__ __forceinline__ RowTile row_tile(const MmParams &p, int tile, int row
 __device__ __forceinline__ int64_t x_row(const MmParams &p, int64_t y_row) { return p.order || p.ids ? (int64_t)p.by_places((uint32_t)y_row) : y_row; }
 __device__ __forceinline__ uint32_t step_of(const MmParams &p, int t) { return p.step_divide ? __umulhi((uint32_t)t, p.step_divide) : (uint32_t)t; }
 
-// The steps of a wave among those that share the columns, begun at another one in every workgroup: rows of X and W are powers of two apart more often than
+// The steps of a part of the columns, begun at another one in every workgroup: rows of X and W are powers of two apart more often than
 // not, and what is read at the same time should not lie in the same channels.
 struct Steps {
     int begin, count, turn, n_tiles;
-    __device__ __forceinline__ Steps(const MmParams &p, int wave, uint32_t workgroup) : n_tiles((int)p.k_tiles)
+    __device__ __forceinline__ Steps(const MmParams &p, int part, int lg_parts, uint32_t workgroup) : n_tiles((int)p.k_tiles)
     {
-        begin = n_tiles * wave >> p.lg_waves;
-        count = (n_tiles * (wave + 1) >> p.lg_waves) - begin;
+        begin = n_tiles * part >> lg_parts;
+        count = (n_tiles * (part + 1) >> lg_parts) - begin;
         turn = (int)((workgroup * 40503u & 0xFFFFu) * (uint32_t)count >> 16);
     }
     __device__ __forceinline__ int operator()(int u) const        // the tile of step u; behind the last one that one; without any, one that is there
@@ -330,23 +332,22 @@ __device__ __forceinline__ void store_sums(const MmParams &p, const RowTile &rt,
 // before the end, where their sums are added in their order.  X comes from the L2 straight into registers, AHEAD_X steps ahead, W AHEAD_W.  CH: chunks of 32
 // columns between applications of a scale (1, 2, or 4).
 // Bound by the reading of W: 64 pairs that meet 40 of 64 matrices of 2816 x 2048 in groups of 64 take 25.8 us, 5.0 TB/s, which is what a large copy reaches.
-// One row times 4096 x 4096 takes 4.5 us on the GPU, of which 3.4 are what any launch takes.
-template <int DT, int CH, bool ZEROS, int NT, int AHEAD_W, int AHEAD_X, int THREADS>
-__global__ void __launch_bounds__(THREADS) q4_split_kernel(const MmParams p)
+// One row times 4096 x 4096 takes 4.6 us on the GPU, of which 2.5 are what any launch takes.
+
+// The sums of the steps of tile_of: 16 rows of X times NT rows of tiles of a matrix from r0 on.  x_at: where this lane's row of X and its columns begin, or
+// kNoRow of one that is not there, which is out of X's range, so that loads of it cost nothing.
+constexpr uint32_t kNoRow = 0xFFFFF000u;
+template <int DT, int CH, bool ZEROS, int NT, int AHEAD_W, int AHEAD_X>
+__device__ __forceinline__ void split_sums(const MmParams &p, int64_t mat, int64_t r0, const Steps &tile_of, uint32_t x_at, int lane, float4v (&acc)[NT])
 {
-    constexpr int kGroups = 4 / CH, kRows = 16;
-    extern __shared__ __attribute__((aligned(16))) float sums[];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n_waves = 1 << p.lg_waves, n = lane & 15, q = lane >> 4;
-    const uint32_t tile = p.by_col_blocks(blockIdx.x), col_block = blockIdx.x - tile * p.col_blocks;
-    const RowTile rt = row_tile(p, tile, kRows);
-    if (rt.count == 0) return;
+    constexpr int kGroups = 4 / CH;
+    const int n = lane & 15, q = lane >> 4;
     const SixteenPlus<DT> sixteen_plus;
-    const int64_t last = p.tile_rows - 1, r0 = (int64_t)col_block * NT;
+    const int64_t last = p.tile_rows - 1;
     const int further = (int)(last - r0 < NT ? last - r0 : NT - 1);
-    const int64_t from = rt.mat * p.tile_rows + r0;
+    const int64_t from = mat * p.tile_rows + r0;
     const char *w_at = reinterpret_cast<const char *>(p.tiles) + from * p.k_tiles * 1024;
     const char *s_at = p.scales + from * p.steps * (32 * kGroups), *z_at = p.zeros + from * p.steps * (16 * kGroups);
-    const Steps tile_of(p, wave, col_block);
     const int n_tiles = tile_of.n_tiles, n_steps = tile_of.count;
 
     uint4v w[AHEAD_W][NT];
@@ -363,9 +364,7 @@ __global__ void __launch_bounds__(THREADS) q4_split_kernel(const MmParams p)
 #pragma unroll
         for (int h = 0; h < NT; ++h) fetch_w(d, h, tile_of(d));
     });
-    // Rows behind the last one are out of X's range: loads of them cost nothing.
     const __amdgpu_buffer_rsrc_t x_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(p.X), 0, (int)p.x_bytes, 0x00020000);
-    const uint32_t x_at = n < rt.count ? (uint32_t)x_row(p, y_row(p, rt.first + n)) * p.ldx_bytes + 16 * q : 0xFFFFF000u;
     auto fetch_x = [&](auto d, int t) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -375,7 +374,6 @@ __global__ void __launch_bounds__(THREADS) q4_split_kernel(const MmParams p)
     };
     static_for<AHEAD_X>([&](auto d) { fetch_x(d, tile_of(d)); });
 
-    float4v acc[NT];
     float taken[NT], of_x = 0.f;                                       // -s (16 + z) and the sum of x of the q-th of four groups
 #pragma unroll
     for (int h = 0; h < NT; ++h) {
@@ -435,13 +433,62 @@ __global__ void __launch_bounds__(THREADS) q4_split_kernel(const MmParams p)
         if (first + d < n_steps) step(d, constant<0>(), constant<(d.value + AHEAD_X < AHEAD_W)>(), first + d);
     });
     if constexpr (CH > 1) take();                                      // what is left of four groups; of the others taken is zero
+}
+
+template <int DT, int CH, bool ZEROS, int NT, int AHEAD_W, int AHEAD_X, int THREADS>
+__global__ void __launch_bounds__(THREADS) q4_split_kernel(const MmParams p)
+{
+    constexpr int kRows = 16;
+    extern __shared__ __attribute__((aligned(16))) float sums[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, q = lane >> 4;
+    const uint32_t tile = p.by_col_blocks(blockIdx.x), col_block = blockIdx.x - tile * p.col_blocks;
+    const RowTile rt = row_tile(p, tile, kRows);
+    if (rt.count == 0) return;
+    const int64_t r0 = (int64_t)col_block * NT;
+    const uint32_t x_at = n < rt.count ? (uint32_t)x_row(p, y_row(p, rt.first + n)) * p.ldx_bytes + 16 * q : kNoRow;
+    float4v acc[NT];
+    split_sums<DT, CH, ZEROS, NT, AHEAD_W, AHEAD_X>(p, rt.mat, r0, Steps(p, wave, p.lg_waves, col_block), x_at, lane, acc);
     float *mine = sums + (int64_t)wave * NT * kRows * kSumRow;
 #pragma unroll
     for (int h = 0; h < NT; ++h)
 #pragma unroll
         for (int i = 0; i < 4; ++i) mine[(h * kRows + 4 * q + i) * kSumRow + n] = acc[h][i];
     __syncthreads();
-    store_sums<DT, NT, kRows>(p, rt, r0, sums, n_waves);
+    store_sums<DT, NT, kRows>(p, rt, r0, sums, 1 << p.lg_waves);
+}
+
+// ---- the products and the weighted sum behind them at once: a row of Y is the sum over a row's pairs of their weights times what their matrices give of the
+// pairs' rows of X.  A workgroup has a row of tiles; each of its waves takes pairs, or parts of their columns where pairs are fewer than waves, and its sums are
+// added in the waves' order.  A launch less, and no results on their way through memory: a layer for one row, 8 of 128 experts of 2 x 768 x 2048 and 2048 x 768,
+// 12.0 us, 15.3 with a product and a sum.  What is left of it are two launches whose reads, 20 MB, take 4 us and follow the calls' latencies.
+constexpr int kSumWaves = 8;
+template <int DT, int CH, bool ZEROS>
+__global__ void __launch_bounds__(64 * kSumWaves) q4_sum_kernel(const MmParams p)
+{
+    __shared__ float sums[kSumWaves][16];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t row = p.by_col_blocks(blockIdx.x), col_block = blockIdx.x - row * p.col_blocks;
+    float sum = 0.f;                                                   // of column lane % 16
+    for (int unit = wave; unit < p.top_k << p.lg_waves; unit += kSumWaves) {
+        const int pair = (int)row * p.top_k + (unit >> p.lg_waves);
+        const int32_t id = p.ids[pair];
+        if ((uint32_t)id >= (uint32_t)p.n_mats) continue;
+        float4v acc[1];
+        split_sums<DT, CH, ZEROS, 1, 4, 2>(p, id, col_block, Steps(p, unit & ((1 << p.lg_waves) - 1), p.lg_waves, blockIdx.x),
+                                           (lane & 15) == 0 ? (uint32_t)pair * p.ldx_bytes + 16 * (lane >> 4) : kNoRow, lane, acc);
+        sum = __builtin_fmaf(p.weights[pair], acc[0][0], sum);         // the first of the sixteen rows, in the first sixteen lanes
+    }
+    if (lane < 16) sums[wave][lane] = sum;
+    __syncthreads();
+    const int64_t col = (int64_t)col_block * 16 + threadIdx.x;
+    if (threadIdx.x >= 16 || col >= p.half) return;
+    float y = 0.f;
+#pragma unroll
+    for (int w = 0; w < kSumWaves; ++w) y += sums[w][threadIdx.x];
+    const int64_t at = row * p.ldy + col;
+    if (p.f32) static_cast<float *>(p.Y)[at] = y;
+    else if (p.bf16) static_cast<__bf16 *>(p.Y)[at] = (__bf16)y;
+    else static_cast<_Float16 *>(p.Y)[at] = (_Float16)y;
 }
 
 // ---- more rows than 16: by products of 32 rows with 32 rows of W, which the matrix units take at 1.4 times the rate of those with 16.  Two rows of tiles are
@@ -572,7 +619,7 @@ __global__ void __launch_bounds__(512) q4_mid_kernel(const MmParams p)
     const RowTile rt = row_tile(p, tile, kRows);
     if (rt.count == 0) return;
     const int64_t r0 = (int64_t)col_block * 4;
-    const Steps tile_of(p, wave, col_block);
+    const Steps tile_of(p, wave, p.lg_waves, col_block);
     const int n_steps = tile_of.count;
     Pairs<DT, CH, ZEROS, MT> pairs(p, rt.mat, r0, lane);
     // rows behind the last one are the first again, and never stored
@@ -806,6 +853,14 @@ Variant mm_variant(int32_t group, bool zeros, const Choice &c)
     return zeros ? mm_variant<DT, 4, true>(c) : mm_variant<DT, 4, false>(c);
 }
 
+template <int DT>
+MmKernel sum_kernel(int32_t group, bool zeros)
+{
+    if (group == 32) return zeros ? q4_sum_kernel<DT, 1, true> : q4_sum_kernel<DT, 1, false>;
+    if (group == 64) return zeros ? q4_sum_kernel<DT, 2, true> : q4_sum_kernel<DT, 2, false>;
+    return zeros ? q4_sum_kernel<DT, 4, true> : q4_sum_kernel<DT, 4, false>;
+}
+
 bool aligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 
 int launched()
@@ -1012,6 +1067,7 @@ extern "C" int q4_mm_routed(const q4_t *h, const void *plan_dev, int64_t n_pairs
 
 namespace {
 
+constexpr int64_t kAgain = 32 << 20;          // bytes read again that cost what the grouping does
 struct Work {
     int64_t h, y, total;           // byte offsets in the work buffer, behind a plan
 };
@@ -1027,6 +1083,38 @@ Work experts_work(const q4_t *up, const q4_t *down, int64_t n_pairs)
     w.y = (w.h + n_pairs * up->rows() * 2 + 255) / 256 * 256;
     w.total = w.y + n_pairs * down->n_rows * 4;
     return w;
+}
+
+// Few pairs are not grouped: each is a tile of its own.  That saves two launches and reads a matrix again for every further pair of it, of which there are
+// k^2 T (T - 1) / 2 E if no expert is chosen more often than others.  In us, grouped and not, where that is so many bytes:
+//   8 of 128 experts of 2048 x 768: 2 rows, 1 MB: 23.5 and 14.9; 6, 17 MB: 36.2 and 30.9; 8, 33 MB: 41.1 and 38.8; 10, 52 MB: 45.2 and 46.5
+//   8 of 256 of 2048 x 512: 12 rows, 26 MB: 43.2 and 39.4; 16, 46 MB: 49.9 and 50.7      2 of 8 of 4096 x 14336: 2 rows, 43 MB: 74.1 and 77.7
+//   6 of 64 of 512 x 256, which stay in the cache: 24 rows, 30 MB: 17.5 and 14.7; 32, 54 MB: 17.6 and 17.4
+// 256 pairs are as many as were measured (8 of 512 of 512 x 256, 12 MB: 26.5 and 18.9).
+bool ungrouped(const q4_t *up, const q4_t *down, int64_t n_rows, int32_t top_k)
+{
+    const int64_t n_pairs = n_rows * top_k;
+    if (n_rows == 1) return true;
+    return n_pairs <= 256 && n_pairs * (n_pairs - top_k) / 2 * ((up->total() + down->total()) / up->n_mats) <= kAgain * up->n_mats;
+}
+
+int sum_pairs(const q4_t *h, const int32_t *ids_dev, const float *weights_dev, int64_t n_rows, int32_t top_k, const void *X_dev, void *Y_dev, int64_t ldy, int32_t y_type, void *hip_stream)
+{
+    MmParams p = mm_params(h, X_dev, h->n_cols, n_rows * top_k, Y_dev, ldy, n_rows);
+    p.ids = ids_dev;
+    p.n_mats = (int32_t)h->n_mats;
+    p.weights = weights_dev;
+    p.top_k = top_k;
+    p.f32 = y_type == VBR_F32;
+    p.bf16 = y_type == VBR_BF16;
+    while (top_k << p.lg_waves < kSumWaves) ++p.lg_waves;
+    p.col_blocks = (int32_t)p.tile_rows;
+    p.by_col_blocks = Divide::by(p.col_blocks);
+    const int64_t grid = n_rows * p.col_blocks;
+    if (grid > kMostThreads / (64 * kSumWaves) || grid > INT32_MAX) return VBR_EUNSUPPORTED;
+    const MmKernel kernel = h->dtype == VBR_F16 ? sum_kernel<VBR_F16>(h->group, h->zeros) : sum_kernel<VBR_BF16>(h->group, h->zeros);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64 * kSumWaves), 0, static_cast<hipStream_t>(hip_stream), p);
+    return launched();
 }
 
 }  // namespace
@@ -1050,11 +1138,11 @@ extern "C" int experts_forward(const q4_t *up, const q4_t *down, const void *X_d
     char *d = static_cast<char *>(work_dev);
     int rc = mm_args(up, X_dev, ldx, d + w.h, up->rows(), up->dtype, n_pairs);
     if (rc != VBR_OK) return rc;
-    // One row needs no grouping: each of its pairs is a tile (the layer for one row, 8 of 128 experts of 2048 x 1536: 24.6 us with a plan).
-    const int32_t *direct = n_rows == 1 ? ids_dev : nullptr;
+    const int32_t *direct = ungrouped(up, down, n_rows, top_k) ? ids_dev : nullptr;
     if (!direct) rc = route_plan(ids_dev, n_pairs, (int32_t)up->n_mats, work_dev, hip_stream);
     if (rc == VBR_OK) rc = mm_pairs(up, work_dev, direct, n_pairs, X_dev, ldx, n_rows, d + w.h, up->rows(), up->dtype, hip_stream);
-    if (rc == VBR_OK) rc = mm_pairs(down, work_dev, direct, n_pairs, d + w.h, up->rows(), n_pairs, d + w.y, down->n_rows, VBR_F32, hip_stream);
+    if (direct) return rc == VBR_OK ? sum_pairs(down, ids_dev, weights_dev, n_rows, top_k, d + w.h, out_dev, ldo, out_type, hip_stream) : rc;
+    if (rc == VBR_OK) rc = mm_pairs(down, work_dev, nullptr, n_pairs, d + w.h, up->rows(), n_pairs, d + w.y, down->n_rows, VBR_F32, hip_stream);
     if (rc == VBR_OK) rc = route_combine(d + w.y, down->n_rows, VBR_F32, ids_dev, weights_dev, n_rows, top_k, (int32_t)up->n_mats, down->n_rows, out_dev, ldo, out_type, hip_stream);
     return rc;
 }

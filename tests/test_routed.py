@@ -598,6 +598,64 @@ def test_a_layer_of_experts(T):
     assert bool((out[T // 2] == 0).all())
 
 
+def numbers(m, e, group):
+    """|s (c - z)| of matrix e"""
+    c = m[0][e].numpy()
+    codes = np.empty((c.shape[0], 2 * c.shape[1]))
+    codes[:, 0::2], codes[:, 1::2] = c & 15, c >> 4
+    by = np.arange(codes.shape[1]) // group
+    return np.abs(np64(m[1][e])[:, by] * (codes - (8 if m[2] is None else np64(m[2][e])[:, by])))
+
+
+# few pairs, which are not grouped: one to many of a row, parts of columns and waves without any, odd sizes, the last two on both sides of where they are
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,k,E,K,F,group,dtype,zeros,out_type", [
+    (1, 1, 1, 32, 32, 32, "bf16", True, "bf16"), (1, 8, 16, 256, 160, 64, "f16", True, "f32"), (1, 2, 3, 96, 1056, 128, "bf16", False, "f32"),
+    (1, 64, 64, 64, 32, 32, "f16", False, "f16"), (2, 3, 40, 288, 416, 32, "f16", True, "bf16"), (3, 2, 30, 544, 96, 256, "bf16", True, "f16"),
+    (1, 4, 9, 64, 4128, 64, "bf16", False, "bf16"), (13, 10, 200, 64, 64, 64, "bf16", True, "f32"), (51, 5, 1024, 32, 32, 32, "f16", False, "f16"),
+    (52, 5, 1024, 32, 32, 32, "f16", False, "f16")])
+def test_a_layer_for_few_rows(T, k, E, K, F, group, dtype, zeros, out_type):
+    t, to = TYPES[dtype], TYPES[out_type]
+    gen = torch.Generator().manual_seed(T * k + E)
+    up, down = matrices(gen, E, 2 * F, K, group, t, zeros), matrices(gen, E, K, F, group, t, zeros)
+    on_up, on_down = [routed.Q4(*[None if a is None else a.to(DEV) for a in q], group=group, gated=g).upload() for q, g in ((up, True), (down, False))]
+    x, weights = torch.randn((T, K), generator=gen).to(t), torch.randn((T, k), generator=gen)
+    ids = torch.randint(0, E, (T, k), generator=gen, dtype=torch.int32)             # the same one twice, too
+    ids = torch.where(torch.rand((T, k), generator=gen) < 0.2, torch.tensor(-1 if T % 2 else E, dtype=torch.int32), ids)
+    if T > 2:
+        ids[1] = E + 5                                                              # a row of none
+    wide = torch.full((T, K + 16), 7.0, dtype=to, device=DEV)
+    out = routed.experts_forward(x.to(DEV), ids.to(DEV), weights.to(DEV), on_up, on_down, wide[:, 8: 8 + K])
+    i64, w64, x64 = ids.numpy(), np64(weights), np64(x)
+    want, tol = np.zeros((T, K)), np.zeros((T, K))
+    for e in range(E):
+        at, place = np.nonzero(i64 == e)
+        if len(at):
+            h, th = gated(*product(x64[at], up, e, group))
+            th = th + half_step(t) * (np.abs(h) + th) + (2.0 ** -25 if dtype == "f16" else 0)       # kept in the matrices' type
+            y, ty = product(h, down, e, group)
+            ty = 1.01 * ty + th @ numbers(down, e, group).T
+            # the sum: a product with the weight and at most k additions, each rounded, of terms no larger than all together
+            np.add.at(want, at, w64[at, place][:, None] * y)
+            np.add.at(tol, at, np.abs(w64[at, place][:, None]) * (ty + (k + 8) * U * (np.abs(y) + ty)))
+    assert_close(out, want, tol, to)
+    assert bool((wide[:, :8] == 7).all()) and bool((wide[:, 8 + K:] == 7).all())
+    # in a graph, twice, with other work between
+    static = [a.to(DEV) for a in (x, ids, weights)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        routed.experts_forward(*static, on_up, on_down)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        again = routed.experts_forward(*static, on_up, on_down)
+    for _ in range(2):
+        again.fill_(3.0)
+        graph.replay()
+        assert torch.equal(again, routed.experts_forward(*static, on_up, on_down))
+
+
 @pytest.mark.gpu
 def test_a_layer_in_a_graph_and_on_other_streams():
     E, k, K, F, group, t, T = 16, 4, 256, 128, 64, torch.float16, 37
