@@ -137,6 +137,7 @@ struct MmParams {
     int32_t gated, f32, fours;                 // fours: four elements of Y from a multiple of four on are aligned to as much
     int32_t col_blocks;                        // of the launch: workgroup i has tile of rows i / col_blocks
     Divide by_col_blocks;
+    int32_t follow;                            // of a plan's tiles: an XCD has some that follow each other
     // routed, or null
     const PlanTile *plan_tiles;
     const int32_t *order;
@@ -752,7 +753,15 @@ __global__ void __launch_bounds__(256, 2) q4_many_kernel(const MmParams p)
     __shared__ int64_t y_lds[kRows];                                             // where the rows of Y begin
     uint4v(*x_lds)[kRows * 16] = reinterpret_cast<uint4v(*)[kRows * 16]>(lds);   // chunk c of row r at r * 16 + (c ^ r % 16)
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
-    const uint32_t tile = p.by_col_blocks(blockIdx.x), col_block = blockIdx.x - tile * p.col_blocks;
+    // Workgroups go to the eight XCDs in turn.  Where an expert has few tiles, each XCD gets some that follow each other, whose rows of X, and of their expert's W,
+    // its L2 then reads once.  Else each XCD has some columns of Y in turn, and their W.
+    uint32_t place = blockIdx.x;
+    if (p.follow) {
+        const uint32_t work = (uint32_t)p.plan_tiles[0].n_tiles * (uint32_t)p.col_blocks, share = (work + 7) / 8;
+        place = (blockIdx.x & 7) * share + (blockIdx.x >> 3);
+        if (blockIdx.x >> 3 >= share || place >= work) return;
+    }
+    const uint32_t tile = p.by_col_blocks(place), col_block = place - tile * p.col_blocks;
     const RowTile rt = row_tile(p, tile, kRows);
     if (rt.count == 0) return;
     const int64_t r0 = ((int64_t)col_block * 4 + wave) * 4;
@@ -950,7 +959,10 @@ int launch_mm(const q4 *h, MmParams &p, int32_t rows, int64_t row_tiles, int64_t
     p.col_blocks = (int32_t)((p.tile_rows + v.tile_rows - 1) / v.tile_rows);
     p.by_col_blocks = Divide::by(p.col_blocks);
     p.lg_waves = __builtin_ctz(v.threads / 64);
-    const int64_t grid = row_tiles * p.col_blocks;
+    // Tiles that follow each other, in us: 64 experts of 2816 x 2048 with 48 rows each 79, in turn 86, with 128 169 and 177; of 2048 x 1408 with 128 93 and 94;
+    // 128 of 1536 x 2048 with 64 106 and 112; 16 of 4096 x 4096 with 256 194 and 196; 8 of 14336 x 4096 with 512 615 and 588
+    p.follow = p.order && c.nt == 16 && rows_each <= 256;
+    const int64_t work = row_tiles * p.col_blocks, grid = p.follow ? (work + 7) / 8 * 8 : work;
     if (grid > kMostThreads / v.threads || grid > INT32_MAX) return VBR_EUNSUPPORTED;
     hipLaunchKernelGGL(v.kernel, dim3((unsigned)grid), dim3(v.threads), v.lds, static_cast<hipStream_t>(hip_stream), p);
     return launched();

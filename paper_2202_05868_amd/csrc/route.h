@@ -32,7 +32,7 @@ struct Divide {
 // Byte offsets in a plan: int32 offsets [n_experts + 1] at 0, int32 order [n_pairs], PlanTile tiles [n_tiles],
 // int32 counts [n_parts][n_experts].
 struct PlanTile {
-    int32_t expert, first, count, unused;          // positions first .. first + count - 1 of the order; count 0: no tile
+    int32_t expert, first, count, n_tiles;         // positions first .. first + count - 1 of the order; count 0: no tile; how many there are
 };
 struct PlanParts {
     int64_t order, tiles, counts, total;

@@ -771,7 +771,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const PlanParams p)
     }
     // the tiles, and what is behind the last pair, by all workgroups
     for (int64_t i = blockIdx.x * (int64_t)kPlanThreads + threadIdx.x; i < p.n_tiles; i += (int64_t)p.n_parts * kPlanThreads) {
-        PlanTile t = {0, 0, 0, 0};
+        PlanTile t = {0, 0, 0, total.y};
         if (i < total.y) {
             int lo = 0, hi = p.n_experts;          // the last expert that begins at or before tile i and has one
             while (hi - lo > 1) {
