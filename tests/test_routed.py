@@ -458,6 +458,35 @@ def test_routed_products(case, a_pair, kind):
     assert_close(y, want, tol, y_type)
 
 
+# as many tiles and columns as fill the GPU: experts of many tiles and of few, tiles that most of the plan's places are not needed for
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,k,E,N,K,group,dtype,zeros,gate", [
+    (2400, 1, 3, 3000, 64, 32, "f16", True, False), (2000, 4, 100, 2100, 96, 64, "bf16", False, True), (800, 4, 200, 1500, 160, 128, "bf16", True, False),
+    (300, 4, 24, 4100, 1056, 128, "f16", False, True), (100, 4, 24, 4100, 288, 32, "bf16", True, False)])
+@pytest.mark.parametrize("kind", ["spread", "few", "none"])
+def test_routed_products_that_fill(T, k, E, N, K, group, dtype, zeros, gate, kind):
+    t = TYPES[dtype]
+    gen = torch.Generator().manual_seed(T + N)
+    q = matrices(gen, E, N, K, group, t, zeros)
+    x = torch.randn((T, K), generator=gen).to(t)
+    ids = torch.randint(0, E, (T, k), generator=gen, dtype=torch.int32)
+    if kind == "few":
+        ids = torch.where(ids % 3 == 1, ids, torch.tensor(E, dtype=torch.int32))
+    if kind == "none":
+        ids[:] = -1
+    m = routed.Q4(*[None if a is None else a.to(DEV) for a in q], group=group, gated=gate).upload()
+    y = torch.full((T * k, m.n_out), 7.0, dtype=t, device=DEV)
+    m.mm_routed(x.to(DEV), routed.route_plan(ids.to(DEV), E), y)
+    flat, x64 = ids.reshape(-1).numpy(), np.repeat(np64(x), k, axis=0)
+    want, tol = np.full((T * k, m.n_out), 7.0), np.zeros((T * k, m.n_out))
+    for e in range(E):
+        at = np.nonzero(flat == e)[0]
+        if len(at):
+            a, b = product(x64[at], q, e, group)
+            want[at], tol[at] = gated(a, b) if gate else (a, b)
+    assert_close(y, want, tol, t)
+
+
 @pytest.mark.gpu
 def test_a_row_with_nan_stays_alone():
     gen = torch.Generator().manual_seed(5)
