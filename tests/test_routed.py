@@ -823,6 +823,18 @@ def test_matrices_and_products_refuse_on_the_host():
     lib.q4_free(h)
 
 
+def test_types_of_results_are_refused_on_the_host():
+    ids, w, y = torch.zeros((4, 2), dtype=torch.int32), torch.zeros((4, 2)), torch.zeros((8, 16))
+    for kw in (dict(out_dtype=torch.float64), dict(out_dtype=torch.float16, out=torch.zeros((4, 16))), dict(out=torch.zeros((4, 16), dtype=torch.float64))):
+        with pytest.raises(ValueError):
+            routed.route_combine(y, ids, w, **kw)
+    m = routed.Q4(torch.zeros((6, 64), dtype=torch.uint8), torch.zeros((6, 2), dtype=torch.float16), group=64)
+    x = torch.zeros((3, 128), dtype=torch.float16)
+    for kw in (dict(y_dtype=torch.bfloat16), dict(y_dtype=torch.float64), dict(y_dtype=torch.float32, y=torch.zeros((3, 6), dtype=torch.float16))):
+        with pytest.raises(ValueError):
+            m.mm(x, **kw)
+
+
 @pytest.mark.gpu
 def test_products_refuse_on_the_gpu():
     codes, scales = torch.zeros((2, 6, 64), dtype=torch.uint8, device=DEV), torch.zeros((2, 6, 2), dtype=torch.float16, device=DEV)
