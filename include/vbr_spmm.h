@@ -375,7 +375,8 @@ void q4_free(q4_t *h);
  * matrix of the expert, D those of down: route_plan, q4_mm_routed twice and route_combine in turn.  up is gated and gives as many columns as down takes,
  * both have as many matrices and one dtype, and down's rows are a multiple of 8.  h is rounded to dtype, which the second product multiplies; its results stay in fp32 until
  * they are summed.  Operands as in those calls; work_dev: caller-allocated, experts_work_bytes bytes (0 for sizes that do not fit), 256-byte
- * aligned, of this call alone while it runs.  For one row the pairs are multiplied as they stand, without a plan.
+ * aligned, of this call alone while it runs.  Few pairs, by the sizes alone, are multiplied as they stand, without a plan, and added up by the second product: the
+ * sum of a row is then taken in another order.
  */
 int64_t experts_work_bytes(const q4_t *up, const q4_t *down, int64_t n_rows, int32_t top_k);
 int experts_forward(const q4_t *up, const q4_t *down, const void *X_dev, int64_t ldx, int64_t n_rows, const int32_t *ids_dev,

@@ -542,6 +542,21 @@ def test_rows_of_x_beyond_4_gib(T):
 
 
 @pytest.mark.gpu
+def test_a_layer_for_rows_beyond_4_gib():
+    T, k, E, K, F, t = 3, 2, 5, 64, 32, torch.bfloat16
+    ld = 2 ** 31 // T // 8 * 8 + 64
+    gen = torch.Generator().manual_seed(2)
+    up, down = matrices(gen, E, 2 * F, K, 32, t, True), matrices(gen, E, K, F, 32, t, True)
+    on = [routed.Q4(*[a.to(DEV) for a in q], group=32, gated=g).upload() for q, g in ((up, True), (down, False))]
+    x, w = torch.randn((T, K), generator=gen).to(t), torch.randn((T, k), generator=gen)
+    far = torch.empty(T * ld, dtype=t, device=DEV).as_strided((T, K), (ld, 1))
+    far.copy_(x.to(DEV))
+    ids = torch.randint(0, E, (T, k), generator=gen, dtype=torch.int32)
+    want, tol = layer_of(np64(x), ids.numpy(), np64(w), up, down, 32, t)
+    assert_close(routed.experts_forward(far, ids.to(DEV), w.to(DEV), *on), want, tol, t)
+
+
+@pytest.mark.gpu
 def test_codes_that_begin_between_words():
     gen = torch.Generator().manual_seed(8)
     q = matrices(gen, 1, 50, 160, 32, torch.float16, True)
@@ -636,6 +651,23 @@ def numbers(m, e, group):
     return np.abs(np64(m[1][e])[:, by] * (codes - (8 if m[2] is None else np64(m[2][e])[:, by])))
 
 
+def layer_of(x, ids, weights, up, down, group, dtype):
+    """What a layer gives, and its bound."""
+    T, k, K = len(x), ids.shape[1], down[0].shape[1]
+    want, tol = np.zeros((T, K)), np.zeros((T, K))
+    for e in range(up[0].shape[0]):
+        at, place = np.nonzero(ids == e)
+        if len(at):
+            h, th = gated(*product(x[at], up, e, group))
+            th = th + half_step(dtype) * (np.abs(h) + th) + (2.0 ** -25 if dtype is torch.float16 else 0)        # kept in the matrices' type
+            y, ty = product(h, down, e, group)
+            ty = 1.01 * ty + th @ numbers(down, e, group).T
+            # the sum: a product with the weight and at most k additions, each rounded, of terms no larger than all together
+            np.add.at(want, at, weights[at, place][:, None] * y)
+            np.add.at(tol, at, np.abs(weights[at, place][:, None]) * (ty + (k + 8) * U * (np.abs(y) + ty)))
+    return want, tol
+
+
 # few pairs, which are not grouped: one to many of a row, parts of columns and waves without any, odd sizes, the last two on both sides of where they are
 @pytest.mark.gpu
 @pytest.mark.parametrize("T,k,E,K,F,group,dtype,zeros,out_type", [
@@ -656,17 +688,7 @@ def test_a_layer_for_few_rows(T, k, E, K, F, group, dtype, zeros, out_type):
     wide = torch.full((T, K + 16), 7.0, dtype=to, device=DEV)
     out = routed.experts_forward(x.to(DEV), ids.to(DEV), weights.to(DEV), on_up, on_down, wide[:, 8: 8 + K])
     i64, w64, x64 = ids.numpy(), np64(weights), np64(x)
-    want, tol = np.zeros((T, K)), np.zeros((T, K))
-    for e in range(E):
-        at, place = np.nonzero(i64 == e)
-        if len(at):
-            h, th = gated(*product(x64[at], up, e, group))
-            th = th + half_step(t) * (np.abs(h) + th) + (2.0 ** -25 if dtype == "f16" else 0)       # kept in the matrices' type
-            y, ty = product(h, down, e, group)
-            ty = 1.01 * ty + th @ numbers(down, e, group).T
-            # the sum: a product with the weight and at most k additions, each rounded, of terms no larger than all together
-            np.add.at(want, at, w64[at, place][:, None] * y)
-            np.add.at(tol, at, np.abs(w64[at, place][:, None]) * (ty + (k + 8) * U * (np.abs(y) + ty)))
+    want, tol = layer_of(x64, i64, w64, up, down, group, t)
     assert_close(out, want, tol, to)
     assert bool((wide[:, :8] == 7).all()) and bool((wide[:, 8 + K:] == 7).all())
     # in a graph, twice, with other work between
