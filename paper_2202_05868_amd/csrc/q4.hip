@@ -185,16 +185,6 @@ struct Words {
     __device__ __forceinline__ float scale(int i) const { return as_f32<DT>((uint16_t)(s >> (N > 1 ? 16 * i : 0))); }
     __device__ __forceinline__ float minus_sixteen_plus_zero(int i) const { return -16.f - (float)(uint8_t)(z >> (N > 1 ? 8 * i : 0)); }
 };
-template <int N, bool ZEROS>
-__device__ __forceinline__ Words<N> load_words(const MmParams &p, int64_t row, int64_t step, int n)
-{
-    const int64_t at = (row * p.steps + step) * 16 + n;
-    Words<N> w{};
-    w.s = reinterpret_cast<const typename Words<N>::Scales *>(p.scales)[at];
-    if constexpr (ZEROS) w.z = reinterpret_cast<const typename Words<N>::Zeros *>(p.zeros)[at];
-    return w;
-}
-
 // x / (1 + exp(-x)).  exp(-x) is 2^t (1 + r), r what rounding took from t = -x log2(e): a relative error of a few steps however large x is.
 __device__ __forceinline__ float silu(float x)
 {
