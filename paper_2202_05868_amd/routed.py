@@ -127,12 +127,11 @@ class RoutePlan:
 
     @property
     def offsets(self):
-        return self._buf[: 4 * (self.n_experts + 1)].view(torch.int32)
+        return self._buf.as_strided((self.n_experts + 1,), (1,), 0)
 
     @property
     def order(self):
-        at = int(_lib.route_plan_order(self.n_pairs, self.n_experts))
-        return self._buf[at: at + 4 * self.n_pairs].view(torch.int32)
+        return self._buf.as_strided((self.n_pairs,), (1,), _lib.route_plan_order(self.n_pairs, self.n_experts) // 4)
 
 
 @lru_cache(maxsize=1024)
@@ -151,7 +150,7 @@ def route_plan(ids, n_experts) -> RoutePlan:
     _dense(what, "ids", ids, ids.shape, torch.int32)
     n_rows, k = ids.shape
     n_experts = int(n_experts)
-    buf = torch.empty(_plan_bytes(n_rows * k, n_experts), dtype=torch.uint8, device=ids.device)
+    buf = torch.empty(_plan_bytes(n_rows * k, n_experts) // 4, dtype=torch.int32, device=ids.device)
     plan = RoutePlan(buf, n_rows, k, n_experts)
     _call(what, _lib.route_plan, ids.get_device(), ids.data_ptr(), n_rows * k, n_experts, plan._at)
     return plan
