@@ -941,9 +941,25 @@ void set_y(MmParams &p, int32_t y_type)
     p.fours = p.ldy % 4 == 0 && aligned(p.Y, p.f32 ? 16 : 8);
 }
 
+// Rows of a tile of one matrix's product.  Large ones make numbers of W less often, small ones fill the GPU sooner.  In us with tiles of 16, 32 and 64 rows:
+//   16 where that makes up to 1024 pieces of 16 x 16: 64 rows, 4096 x 1024 (256 pieces) 7.4 10.9 16.0; 128 rows, 1024 x 1024 (512) 4.5 6.5 8.6; 32 rows, 8192 x 8192
+//   (1024) 16.7 17.7; 64 rows, 4096 x 4096 (1024) 10.0 11.6 16.4; 80 rows (1280) 15.2 11.7 16.5
+//   32 where that makes up to 256 workgroups of 32 x 64, one a CU, or 512 and either 64 rows make more than 256 too or columns are few: 128 rows, 4096 x 4096 (256) 15.7
+//   12.4 16.8; 160 rows, 4096 x 6144 (480, and 288) 26.6 17.6 25.2; 512 rows, 2048 x 2048 (512, and 256) 16.9 11.5 13.0; 192 rows, 14336 x 4096 (384, and
+//   192) - 46.9 41.6; 128 rows, 8192 x 8192 (512, and 256) 47 31 29; 192 rows, 4096 x 6144 (576) 32 22.7 25.3; 128 rows, 4096 x 14336 (896) 46 31 27
+//   and for 65 to 96 rows, of which 64 would make 128: 80 rows, 4096 x 14336 (672) 33 22.9 26.5; 96 rows, 2048 x 32768 (1536) 41 27.8 29.5
+int32_t mm_tile_rows(const MmParams &p, int64_t n_rows)
+{
+    const auto tiles = [n_rows](int32_t rows) { return (n_rows + rows - 1) / rows; };
+    if (p.x_bytes != 0 && (n_rows <= 16 || tiles(16) * p.tile_rows <= 1024)) return 16;      // (an X of 4 GiB and more: the other kernels have 64-bit addresses)
+    const int64_t side = (p.tile_rows + 3) / 4, of_32 = tiles(32) * side, of_64 = tiles(64) * side;
+    if (n_rows <= 32 || (n_rows > 64 && n_rows <= 96) || of_32 <= 256 || (of_32 <= 512 && (of_64 > 256 || p.k_tiles <= 32))) return 32;
+    return 64;
+}
+
 int launch_mm(const q4 *h, MmParams &p, int32_t rows, int64_t row_tiles, int64_t rows_each, void *hip_stream)
 {
-    if (rows == 16 && p.x_bytes == 0) rows = 32;       // an X of 4 GiB and more: the other kernels have 64-bit addresses
+    if (rows == 16 && p.x_bytes == 0) rows = 32;       // (of a plan's tiles, or of rows one by one: there are as many)
     const Choice c = choose(p, rows, row_tiles, rows_each, h->n_mats);
     const Variant v = h->dtype == VBR_F16 ? mm_variant<VBR_F16>(h->group, h->zeros, c) : mm_variant<VBR_BF16>(h->group, h->zeros, c);
     p.col_blocks = (int32_t)((p.tile_rows + v.tile_rows - 1) / v.tile_rows);
@@ -1034,7 +1050,7 @@ extern "C" int q4_mm(const q4_t *h, const void *X_dev, int64_t ldx, void *Y_dev,
     if (n_rows == 0) return VBR_OK;
     MmParams p = mm_params(h, X_dev, ldx, n_rows, Y_dev, ldy, n_rows);
     set_y(p, y_type);
-    const int32_t rows = n_rows <= 16 ? 16 : n_rows <= 32 ? 32 : 64;
+    const int32_t rows = mm_tile_rows(p, n_rows);
     return launch_mm(h, p, rows, (n_rows + rows - 1) / rows, n_rows, hip_stream);
 }
 

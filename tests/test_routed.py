@@ -406,6 +406,28 @@ def test_products_with_one_matrix(case, out):
     assert bool((y[0] == 7).all()) and bool((y[T + 1] == 7).all()) and bool((y[:, :3] == 7).all()) and bool((y[:, 3 + m.n_out:] == 7).all())
 
 
+# on both sides of where tiles of 16, 32 and 64 rows begin
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,N,K,group,dtype,zeros,gate", [
+    (17, 520, 96, 32, "bf16", True, False), (33, 8176, 160, 64, "f16", False, False), (48, 5456, 288, 128, "bf16", True, True), (64, 4097, 416, 32, "f16", True, False),
+    (1024, 256, 1056, 128, "bf16", True, False), (1025, 256, 96, 64, "f16", True, True), (40, 16384, 224, 128, "bf16", False, False), (40, 16400, 224, 32, "bf16", True, False),
+    (96, 11000, 160, 64, "bf16", True, True), (97, 11000, 160, 64, "f16", True, False), (65, 20000, 64, 32, "f16", False, False), (512, 2048, 2080, 256, "bf16", True, False),
+    (513, 2048, 544, 128, "f16", False, True), (160, 6144, 640, 128, "bf16", True, False)])
+def test_products_where_tiles_change(T, N, K, group, dtype, zeros, gate):
+    t = TYPES[dtype]
+    gen = torch.Generator().manual_seed(T + N)
+    q = matrices(gen, 1, N, K, group, t, zeros)
+    x = torch.randn((T, K), generator=gen).to(t)
+    want, tol = product(np64(x), q, 0, group)
+    if gate:
+        want, tol = gated(want, tol)
+    m = routed.Q4(*[None if a is None else a.to(DEV) for a in q], group=group, gated=gate).upload()
+    y = torch.full((T + 1, m.n_out), 7.0, dtype=torch.float32, device=DEV)
+    m.mm(x.to(DEV), y[:T])
+    assert_close(y[:T], want, tol, torch.float32)
+    assert bool((y[T] == 7).all())
+
+
 ROUTED = [
     # T, k, E, N, K, group, type, zeros, gated
     (1, 1, 1, 16, 32, 32, "f16", False, False),
