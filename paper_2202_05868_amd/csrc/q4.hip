@@ -140,6 +140,7 @@ struct MmParams {
     int32_t follow;                            // of a plan's tiles: an XCD has some that follow each other
     // routed, or null
     const PlanTile *plan_tiles;
+    int32_t lg_parts;                          // of a plan's tile: 2^lg_parts tiles of this product
     const int32_t *order;
     const int32_t *ids;                        // or, of pairs that each have a tile of their own, these and how many matrices there are
     int32_t n_mats;
@@ -231,8 +232,9 @@ struct RowTile {
 __device__ __forceinline__ RowTile row_tile(const MmParams &p, int tile, int rows)      // count 0: none
 {
     if (p.order) {
-        const PlanTile t = p.plan_tiles[tile];
-        return {t.expert, t.first, t.count};
+        const PlanTile t = p.plan_tiles[tile >> p.lg_parts];
+        const int at = (tile & ((1 << p.lg_parts) - 1)) * rows, left = t.count - at;
+        return {t.expert, t.first + at, left < 0 ? 0 : left < rows ? left : rows};
     }
     if (p.ids) {
         const int32_t id = p.ids[tile];
@@ -747,7 +749,7 @@ __global__ void __launch_bounds__(256, 2) q4_many_kernel(const MmParams p)
     // its L2 then reads once.  Else each XCD has some columns of Y in turn, and their W.
     uint32_t place = blockIdx.x;
     if (p.follow) {
-        const uint32_t work = (uint32_t)p.plan_tiles[0].n_tiles * (uint32_t)p.col_blocks, share = (work + 7) / 8;
+        const uint32_t work = ((uint32_t)p.plan_tiles[0].n_tiles << p.lg_parts) * (uint32_t)p.col_blocks, share = (work + 7) / 8;
         place = (blockIdx.x & 7) * share + (blockIdx.x >> 3);
         if (blockIdx.x >> 3 >= share || place >= work) return;
     }
@@ -922,12 +924,13 @@ MmParams mm_params(const q4_t *h, const void *X_dev, int64_t ldx, int64_t x_rows
 //   8192 x 8192, 512 rows of tiles: 14.6 and 12.0).
 //   Eight waves where each has two steps or workgroups are few (T 1, 2048 x 14336: 6.3, four 6.4; T 8, 8192 x 8192: 9.9 and 13.2; 8 pairs, 2048 x 1536: 7.0 and
 //   7.4), four where there are many (64 pairs of 64 experts, 2048 x 2816: 24.8, eight 25.5; 1408 x 2048: 14.9 and 16.2)
+int64_t filled(const MmParams &p, int32_t rows, int64_t n_mats) { return p.n_rows / rows + n_mats / 2; }
+bool many(const MmParams &p, int64_t row_tiles) { return row_tiles * ((p.tile_rows + 15) / 16) >= (p.order ? p.k_tiles <= 4 ? 224 : 384 : 256); }
 Choice choose(const MmParams &p, int32_t rows, int64_t row_tiles, int64_t rows_each, int64_t n_mats)
 {
     const int64_t tiles = row_tiles * p.tile_rows;
     if (rows > 16) {
-        const int64_t filled = p.order ? std::min(row_tiles, p.n_rows / rows + n_mats / 2) : row_tiles;
-        if (filled * ((p.tile_rows + 15) / 16) >= (p.order ? p.k_tiles <= 4 ? 224 : 384 : 256)) return {rows, 16, 4};
+        if (many(p, p.order ? filled(p, rows, n_mats) : row_tiles)) return {rows, 16, 4};
         return {rows, 4, row_tiles * ((p.tile_rows + 3) / 4) <= 256 && p.k_tiles >= 16 ? 8 : 4};
     }
     if (tiles <= 256 && !p.gated) return {16, 1, p.k_tiles >= 32 ? 8 : 4};
@@ -955,6 +958,16 @@ int32_t mm_tile_rows(const MmParams &p, int64_t n_rows)
     const int64_t side = (p.tile_rows + 3) / 4, of_32 = tiles(32) * side, of_64 = tiles(64) * side;
     if (n_rows <= 32 || (n_rows > 64 && n_rows <= 96) || of_32 <= 256 || (of_32 <= 512 && (of_64 > 256 || p.k_tiles <= 32))) return 32;
     return 64;
+}
+
+// Of a plan's product: by the same (16, 32 and 64 rows: 4 experts of 320 x 1280 with 48 rows each 5.5 7.9 10.5; 8 of 1024 x 1024 with 100 11.7 9.0 9.6), tiles that are
+// filled in part counted as for choose(), and no more than a plan's tile has.  And 32 where that makes as many workgroups as the kernel for many wants, and 64 does not:
+// 64 experts of 512 x 512 with 64 rows 10.6 and 15.3; 16 of 1024 x 2048 with 200 28.6 and 33.9; 32 of 1536 x 4096 with 48 49.5 and 46.9.
+int32_t plan_rows(const MmParams &p, int32_t most, int64_t n_mats)
+{
+    if (most == 16 || (p.x_bytes != 0 && filled(p, 16, n_mats) * p.tile_rows <= 1024)) return 16;
+    if (most == 32 || filled(p, 32, n_mats) * ((p.tile_rows + 3) / 4) <= 512) return 32;
+    return many(p, filled(p, 32, n_mats)) && !many(p, filled(p, 64, n_mats)) ? 32 : 64;
 }
 
 int launch_mm(const q4 *h, MmParams &p, int32_t rows, int64_t row_tiles, int64_t rows_each, void *hip_stream)
@@ -1075,7 +1088,9 @@ static int mm_pairs(const q4_t *h, const void *plan_dev, const int32_t *ids_dev,
     const char *d = static_cast<const char *>(plan_dev);
     p.order = reinterpret_cast<const int32_t *>(d + parts.order);
     p.plan_tiles = reinterpret_cast<const PlanTile *>(d + parts.tiles);
-    return launch_mm(h, p, parts.tile_rows, parts.n_tiles, n_pairs / h->n_mats, hip_stream);
+    const int32_t rows = plan_rows(p, parts.tile_rows, h->n_mats);
+    p.lg_parts = __builtin_ctz(parts.tile_rows / rows);
+    return launch_mm(h, p, rows, parts.n_tiles << p.lg_parts, n_pairs / h->n_mats, hip_stream);
 }
 
 extern "C" int q4_mm_routed(const q4_t *h, const void *plan_dev, int64_t n_pairs, const void *X_dev, int64_t ldx, int64_t n_rows, void *Y_dev, int64_t ldy, int32_t y_type, void *hip_stream)

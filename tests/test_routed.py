@@ -484,7 +484,10 @@ def test_routed_products(case, a_pair, kind):
 @pytest.mark.gpu
 @pytest.mark.parametrize("T,k,E,N,K,group,dtype,zeros,gate", [
     (2400, 1, 3, 3000, 64, 32, "f16", True, False), (2000, 4, 100, 2100, 96, 64, "bf16", False, True), (800, 4, 200, 1500, 160, 128, "bf16", True, False),
-    (300, 4, 24, 4100, 1056, 128, "f16", False, True), (100, 4, 24, 4100, 288, 32, "bf16", True, False)])
+    (300, 4, 24, 4100, 1056, 128, "f16", False, True), (100, 4, 24, 4100, 288, 32, "bf16", True, False),
+    # tiles of the plan that the product takes whole, in halves and in quarters
+    (400, 2, 4, 1280, 160, 64, "f16", True, False), (700, 2, 7, 1300, 1056, 128, "bf16", True, True), (700, 2, 7, 700, 160, 32, "bf16", False, False),
+    (200, 2, 4, 320, 288, 128, "bf16", True, True), (60, 2, 4, 320, 2080, 256, "f16", False, False)])
 @pytest.mark.parametrize("kind", ["spread", "few", "none"])
 def test_routed_products_that_fill(T, k, E, N, K, group, dtype, zeros, gate, kind):
     t = TYPES[dtype]
