@@ -921,20 +921,21 @@ MmParams mm_params(const q4_t *h, const void *X_dev, int64_t ldx, int64_t x_rows
 //   8192 x 8192: 11.1 and 9.7).  Else two, and nothing ahead but the next step: then eight waves of a SIMD hide each other's waits (W four steps ahead
 //   takes registers for that; T 1, 8192 x 16384: 15.2 and 21.3; 112 pairs of 28 experts, 576 x 1024: 5.4 and 7.1).  Four rows of tiles, for which X is
 //   read half as often, with more than 8 rows of X and workgroups for every CU still (T 16, 8192 x 16384: 17.8, two 22.1; T 16, 4064 x 10999: 9.6 and 10.5; T 16,
-//   8192 x 8192, 512 rows of tiles: 14.6 and 12.0).
+//   8192 x 8192, 512 rows of tiles: 14.6 and 12.0; five tiles of rows, T 80, 14336 x 2048: 25.5 and 33.2), but with one tile of rows not for groups of 32, where the vector units
+//   have more to do than to wait for X (T 16, 4064 x 10976: 12.9 and 11.5; T 9, 2048 x 16384: 9.3 and 7.9; T 48, 4096 x 4096: 12.3 and 12.8).
 //   Eight waves where each has two steps or workgroups are few (T 1, 2048 x 14336: 6.3, four 6.4; T 8, 8192 x 8192: 9.9 and 13.2; 8 pairs, 2048 x 1536: 7.0 and
 //   7.4), four where there are many (64 pairs of 64 experts, 2048 x 2816: 24.8, eight 25.5; 1408 x 2048: 14.9 and 16.2)
 int64_t filled(const MmParams &p, int32_t rows, int64_t n_mats) { return p.n_rows / rows + n_mats / 2; }
 bool many(const MmParams &p, int64_t row_tiles) { return row_tiles * ((p.tile_rows + 15) / 16) >= (p.order ? p.k_tiles <= 4 ? 224 : 384 : 256); }
-Choice choose(const MmParams &p, int32_t rows, int64_t row_tiles, int64_t rows_each, int64_t n_mats)
+Choice choose(const q4 *h, const MmParams &p, int32_t rows, int64_t row_tiles, int64_t rows_each)
 {
     const int64_t tiles = row_tiles * p.tile_rows;
     if (rows > 16) {
-        if (many(p, p.order ? filled(p, rows, n_mats) : row_tiles)) return {rows, 16, 4};
+        if (many(p, p.order ? filled(p, rows, h->n_mats) : row_tiles)) return {rows, 16, 4};
         return {rows, 4, row_tiles * ((p.tile_rows + 3) / 4) <= 256 && p.k_tiles >= 16 ? 8 : 4};
     }
     if (tiles <= 256 && !p.gated) return {16, 1, p.k_tiles >= 32 ? 8 : 4};
-    if (tiles >= 640 && rows_each > 8) return {16, 4, 4};
+    if (tiles >= 640 && rows_each > 8 && (h->group > 32 || row_tiles > 1)) return {16, 4, 4};
     return {16, 2, (p.k_tiles >= 16 && tiles < 2048) || (p.k_tiles >= 8 && tiles < 1024) ? 8 : 4};
 }
 
@@ -973,7 +974,7 @@ int32_t plan_rows(const MmParams &p, int32_t most, int64_t n_mats)
 int launch_mm(const q4 *h, MmParams &p, int32_t rows, int64_t row_tiles, int64_t rows_each, void *hip_stream)
 {
     if (rows == 16 && p.x_bytes == 0) rows = 32;       // (of a plan's tiles, or of rows one by one: there are as many)
-    const Choice c = choose(p, rows, row_tiles, rows_each, h->n_mats);
+    const Choice c = choose(h, p, rows, row_tiles, rows_each);
     const Variant v = h->dtype == VBR_F16 ? mm_variant<VBR_F16>(h->group, h->zeros, c) : mm_variant<VBR_BF16>(h->group, h->zeros, c);
     p.col_blocks = (int32_t)((p.tile_rows + v.tile_rows - 1) / v.tile_rows);
     p.by_col_blocks = Divide::by(p.col_blocks);

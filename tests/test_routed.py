@@ -412,7 +412,8 @@ def test_products_with_one_matrix(case, out):
     (17, 520, 96, 32, "bf16", True, False), (33, 8176, 160, 64, "f16", False, False), (48, 5456, 288, 128, "bf16", True, True), (64, 4097, 416, 32, "f16", True, False),
     (1024, 256, 1056, 128, "bf16", True, False), (1025, 256, 96, 64, "f16", True, True), (40, 16384, 224, 128, "bf16", False, False), (40, 16400, 224, 32, "bf16", True, False),
     (96, 11000, 160, 64, "bf16", True, True), (97, 11000, 160, 64, "f16", True, False), (65, 20000, 64, 32, "f16", False, False), (512, 2048, 2080, 256, "bf16", True, False),
-    (513, 2048, 544, 128, "f16", False, True), (160, 6144, 640, 128, "bf16", True, False)])
+    (513, 2048, 544, 128, "f16", False, True), (160, 6144, 640, 128, "bf16", True, False), (48, 4000, 288, 32, "bf16", True, False),
+    (33, 4180, 416, 32, "f16", False, True), (12, 12000, 288, 32, "f16", True, True)])
 def test_products_where_tiles_change(T, N, K, group, dtype, zeros, gate):
     t = TYPES[dtype]
     gen = torch.Generator().manual_seed(T + N)
