@@ -186,14 +186,9 @@ struct Words {
     __device__ __forceinline__ float scale(int i) const { return as_f32<DT>((uint16_t)(s >> (N > 1 ? 16 * i : 0))); }
     __device__ __forceinline__ float minus_sixteen_plus_zero(int i) const { return -16.f - (float)(uint8_t)(z >> (N > 1 ? 8 * i : 0)); }
 };
-// x / (1 + exp(-x)).  exp(-x) is 2^t (1 + r), r what rounding took from t = -x log2(e): a relative error of a few steps however large x is.
-__device__ __forceinline__ float silu(float x)
-{
-    constexpr float log2e = 1.44269502f, rest = 1.92596299e-8f, ln2 = 0.693147181f;      // log2(e) in two numbers
-    const float t = -x * log2e, r = __builtin_fmaf(-x, rest, __builtin_fmaf(-x, log2e, -t));
-    const float e = __builtin_amdgcn_exp2f(t);
-    return x * __builtin_amdgcn_rcpf(1.f + __builtin_fmaf(e, r * ln2, e));
-}
+// x / (1 + exp(-x)) for any x, off by eight half steps of its size at most (three of the exponential, two of the reciprocal, one of the sum and of each product): x / (1 + e) or
+// x e / (1 + e) with e = exp(-|x|), which does not overflow.  NaN stays NaN; below -87, where e is below the normal fp32 numbers, it may be zero.
+__device__ __forceinline__ float silu(float x) { return x * sigmoid_of(x); }
 
 template <int DT>
 __device__ __forceinline__ void store_y(const MmParams &p, int64_t at, float y)

@@ -33,20 +33,6 @@ __device__ __forceinline__ void store_f32(void *p, int64_t i, float v)          
     else static_cast<__bf16 *>(p)[i] = (__bf16)v;
 }
 
-// exp(x), x at most a little above 0, within three steps: 2^t (1 + r), r what rounding took from t = x log2(e); 0 for -inf and NaN
-__device__ __forceinline__ float exp_of(float x)
-{
-    constexpr float log2e = 1.44269502f, rest = 1.92596299e-8f, ln2 = 0.693147181f;      // log2(e) in two numbers
-    x = fmaxf(x, -200.f);
-    const float t = x * log2e, r = __builtin_fmaf(x, rest, __builtin_fmaf(x, log2e, -t)), e = __builtin_amdgcn_exp2f(t);
-    return __builtin_fmaf(e, r * ln2, e);
-}
-__device__ __forceinline__ float sigmoid_of(float x)
-{
-    const float e = exp_of(-fabsf(x)), d = __builtin_amdgcn_rcpf(1.f + e);
-    return x < 0.f ? e * d : d;
-}
-
 // LP lanes have a row: all of them get the result.  16 lanes are one row of the vector unit.
 template <int CTRL>
 __device__ __forceinline__ uint32_t from_lane(uint32_t x) { return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, CTRL, 0xf, 0xf, true); }

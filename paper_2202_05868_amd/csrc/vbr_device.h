@@ -34,6 +34,21 @@ __device__ __forceinline__ void dma16(const void *gptr, uint32_t lds_base)
                  "s"((uint32_t)__builtin_amdgcn_readfirstlane(lds_base)) : "memory");
 }
 
+// exp(x), x at most a little above 0, within three half steps: 2^t (1 + r), r what rounding took from t = x log2(e); 0 for -inf and NaN, which count as -200 like all
+// that is lower (t and r of an infinity have no difference).  Not for numbers far above 0: of a power that overflows the last line takes infinity from infinity.
+__device__ __forceinline__ float exp_of(float x)
+{
+    constexpr float log2e = 1.44269502f, rest = 1.92596299e-8f, ln2 = 0.693147181f;      // log2(e) in two numbers
+    x = __builtin_fmaxf(x, -200.f);
+    const float t = x * log2e, r = __builtin_fmaf(x, rest, __builtin_fmaf(x, log2e, -t)), e = __builtin_amdgcn_exp2f(t);
+    return __builtin_fmaf(e, r * ln2, e);
+}
+__device__ __forceinline__ float sigmoid_of(float x)      // of a NaN: 1
+{
+    const float e = exp_of(-__builtin_fabsf(x)), d = __builtin_amdgcn_rcpf(1.f + e);
+    return x < 0.f ? e * d : d;
+}
+
 template <int N>
 __device__ __forceinline__ void wait_vmcnt()
 {

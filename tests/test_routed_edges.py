@@ -1,0 +1,84 @@
+"""Routed products where numbers are far apart or near each other, against the definitions in 64 bits of test_routed."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2202_05868_amd import routed
+from test_routed import DEV, TYPES, assert_close, gated, layer_of, matrices, np64, product
+
+# ------------------------------------------------------------------------------------------- gates
+def far_matrices(gen, M, N, K, group, dtype, zeros):
+    """Gated matrices whose gates' rows are of very different size, so that with x of deviation 1 gates have deviations of 4 .. 4000 and every
+    tenth lies between -89 and -2000; what they gate has a deviation near 0.1, so that results stay in fp16's range."""
+    G, F = -(-K // group), N // 2
+    codes = torch.randint(0, 256, (M, N, K // 2), generator=gen, dtype=torch.uint8)
+    size = torch.full((M, N, 1), 0.1)
+    size[:, :F] = 4 * 1000 ** torch.rand((M, F, 1), generator=gen)
+    scales = ((torch.rand((M, N, G), generator=gen) + 0.5) * size / (4.6 * math.sqrt(K))).to(dtype)
+    z = torch.randint(6, 10, (M, N, G), generator=gen, dtype=torch.uint8) if zeros else None
+    return codes, scales, z
+
+
+def gated_of(x, q, m, group):
+    with np.errstate(over="ignore"):                                        # (1 + an infinite exponential divides to zero)
+        return gated(*product(x, q, m, group))
+
+
+def on_gpu(q, group, gate=True):
+    return routed.Q4(*[None if a is None else a.to(DEV) for a in q], group=group, gated=gate).upload()
+
+
+# products of 16, 32 and 64 rows, in few workgroups and in many
+@pytest.mark.gpu
+@pytest.mark.parametrize("out", ["same", "f32"])
+@pytest.mark.parametrize("T,F,K,group,dtype,zeros", [
+    (1, 66, 160, 64, "bf16", False), (5, 300, 288, 32, "f16", True), (16, 12000, 160, 64, "bf16", True), (48, 5456, 288, 128, "bf16", True), (40, 16384, 96, 128, "f16", False),
+    (130, 16384, 64, 32, "bf16", True), (300, 8192, 160, 128, "f16", True), (70, 24000, 64, 64, "bf16", False), (961, 8200, 96, 128, "bf16", True), (1024, 8200, 64, 32, "f16", False)])
+def test_gates_far_from_zero(T, F, K, group, dtype, zeros, out):
+    t = TYPES[dtype]
+    y_type = t if out == "same" else torch.float32
+    gen = torch.Generator().manual_seed(T + F)
+    q = far_matrices(gen, 1, 2 * F, K, group, t, zeros)
+    x = torch.randn((T, K), generator=gen).to(t)
+    want, tol = gated_of(np64(x), q, 0, group)
+    y = on_gpu(q, group).mm(x.to(DEV), y_dtype=y_type)
+    assert bool(y.isfinite().all())
+    assert_close(y, want, tol, y_type)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,k,E,F,K,group,dtype,zeros", [(16, 4, 64, 34, 160, 32, "bf16", True), (600, 4, 8, 129, 544, 128, "bf16", True), (400, 4, 64, 513, 160, 32, "f16", True),
+                                                         (2000, 4, 64, 257, 224, 64, "f16", False)])
+def test_routed_gates_far_from_zero(T, k, E, F, K, group, dtype, zeros):
+    t = TYPES[dtype]
+    gen = torch.Generator().manual_seed(T + F)
+    q = far_matrices(gen, E, 2 * F, K, group, t, zeros)
+    x = torch.randn((T, K), generator=gen).to(t)
+    ids = torch.randint(0, E, (T, k), generator=gen, dtype=torch.int32)
+    y = on_gpu(q, group).mm_routed(x.to(DEV), routed.route_plan(ids.to(DEV), E))
+    flat, x64 = ids.reshape(-1).numpy(), np.repeat(np64(x), k, axis=0)
+    want, tol = np.zeros((T * k, F)), np.zeros((T * k, F))
+    for e in range(E):
+        at = np.nonzero(flat == e)[0]
+        want[at], tol[at] = gated_of(x64[at], q, e, group)
+    assert bool(y.isfinite().all())
+    assert_close(y, want, tol, t)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("T", [1, 4, 400])
+def test_a_layer_with_gates_far_from_zero(T, dtype):
+    E, k, K, F, group, t = 12, 3, 288, 160, 32, TYPES[dtype]
+    gen = torch.Generator().manual_seed(T)
+    up = far_matrices(gen, E, 2 * F, K, group, t, True)
+    down = matrices(gen, E, K, F, group, t, False)
+    x, w = torch.randn((T, K), generator=gen).to(t), torch.rand((T, k), generator=gen)
+    ids = torch.randint(0, E, (T, k), generator=gen, dtype=torch.int32)
+    with np.errstate(over="ignore"):
+        want, tol = layer_of(np64(x), ids.numpy(), np64(w), up, down, group, t)
+    out = routed.experts_forward(x.to(DEV), ids.to(DEV), w.to(DEV), on_gpu(up, group), on_gpu(down, group, False))
+    assert bool(out.isfinite().all())
+    assert_close(out, want, tol, t)
