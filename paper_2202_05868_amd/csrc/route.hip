@@ -787,26 +787,32 @@ struct CombineParams {
     Divide by_chunks;
 };
 
+using Global = const __attribute__((address_space(1))) char *;
+template <class T>
+__device__ __forceinline__ T load_from(Global p) { return *(const __attribute__((address_space(1))) T *)p; }
+
 template <int TY>
-__device__ __forceinline__ void load8(const void *p, int64_t i, float (&x)[8])
+__device__ __forceinline__ void load8(Global p, float (&x)[8])
 {
     if constexpr (TY == VBR_F32) {
-        const float4v a = *reinterpret_cast<const float4v *>(static_cast<const float *>(p) + i), b = *reinterpret_cast<const float4v *>(static_cast<const float *>(p) + i + 4);
+        const float4v a = load_from<float4v>(p), b = load_from<float4v>(p + 16);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             x[j] = a[j];
             x[j + 4] = b[j];
         }
     } else if constexpr (TY == VBR_F16) {
-        const half8v a = *reinterpret_cast<const half8v *>(static_cast<const _Float16 *>(p) + i);
+        const half8v a = load_from<half8v>(p);
 #pragma unroll
         for (int j = 0; j < 8; ++j) x[j] = (float)a[j];
     } else {
-        const bf16x8v a = *reinterpret_cast<const bf16x8v *>(static_cast<const __bf16 *>(p) + i);
+        const bf16x8v a = load_from<bf16x8v>(p);
 #pragma unroll
         for (int j = 0; j < 8; ++j) x[j] = (float)a[j];
     }
 }
+template <int TY>
+__device__ __forceinline__ Global element(const void *p, int64_t i) { return (Global)p + i * (TY == VBR_F32 ? 4 : 2); }
 
 template <int TY>
 __device__ __forceinline__ void store8(void *p, int64_t i, const float (&x)[8])
@@ -827,8 +833,11 @@ __device__ __forceinline__ void store8(void *p, int64_t i, const float (&x)[8])
     }
 }
 
+// What is read in the place of a result whose pair has no expert, so that loads need no branch: such results are never read, and their rows need not be there.
+__device__ const float4v nothing[2] = {};
+
 // A thread owns eight columns of a row of out; the row's results are added in the order of their places.  Bound by what it reads: 4096 rows of 8 bf16 results of
-// 2048 take 38 us, 4.0 TB/s.  AT places are on their way at a time (of one that does not count, the first one's, without effect).
+// 2048 take 38 us, 4.0 TB/s, from memory (23 where they are in the cache behind the L2).  AT places are on their way at a time.
 template <int TY, int TO, int AT>
 __global__ void __launch_bounds__(kRouteThreads) route_combine_kernel(const CombineParams p)
 {
@@ -849,7 +858,7 @@ __global__ void __launch_bounds__(kRouteThreads) route_combine_kernel(const Comb
             w[u] = p.weights[pair];
         }
 #pragma unroll
-        for (int u = 0; u < AT; ++u) load8<TY>(p.y, (there[u] ? first + j0 + u : first) * p.ldy + col, x[u]);
+        for (int u = 0; u < AT; ++u) load8<TY>(there[u] ? element<TY>(p.y, (first + j0 + u) * p.ldy + col) : (Global)nothing, x[u]);
 #pragma unroll
         for (int u = 0; u < AT; ++u)
 #pragma unroll
@@ -872,9 +881,9 @@ __global__ void __launch_bounds__(kRouteThreads) route_combine_grad_kernel(const
     float dot = 0.f;
     for (int col = lane * 8; col < p.n_cols; col += 512) {
         float g[8], x[8];
-        load8<TO>(p.dout, row * p.ldo + col, g);
+        load8<TO>(element<TO>(p.dout, row * p.ldo + col), g);
         if (there) {
-            load8<TY>(p.y, pair * p.ldy + col, x);
+            load8<TY>(element<TY>(p.y, pair * p.ldy + col), x);
 #pragma unroll
             for (int i = 0; i < 8; ++i) dot = __builtin_fmaf(g[i], x[i], dot);
         }
@@ -1148,8 +1157,8 @@ extern "C" int route_combine(const void *y_dev, int64_t ldy, int32_t y_type, con
     const int64_t grid = (n_rows * p.n_chunks + kRouteThreads - 1) / kRouteThreads;
     if (grid > kMostThreads / 2 / kRouteThreads) return VBR_EUNSUPPORTED;          // (threads are divided by n_chunks in 31 bits)
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    // two places at a time, or eight where there are as many (in us; 16384 fp32 results of 2048 columns, 8 a row: 24.8, with two 26.4; 6 a row: 28.8 and 26.6;
-    // one a row: 85.8 and 46.7, since what is not there is read as well)
+    // two places at a time, or eight where there are as many (in us, results in the cache; 16384 fp32 results of 2048 columns, 8 a row: 22.8, with two 22.9; 6 a row:
+    // 24.0 and 23.9; one a row: 53.7 and 40.7)
     if (top_k < 8) COMBINE_BY_TYPES(route_combine_2);
     else COMBINE_BY_TYPES(route_combine_8);
     return launched();

@@ -6,7 +6,8 @@ import pytest
 import torch
 
 from paper_2202_05868_amd import routed
-from test_routed import DEV, TYPES, assert_close, gated, layer_of, matrices, np64, product
+from test_routed import DEV, TYPES, U, assert_close, gated, layer_of, matrices, np64, product
+
 
 # ------------------------------------------------------------------------------------------- gates
 def far_matrices(gen, M, N, K, group, dtype, zeros):
@@ -82,3 +83,24 @@ def test_a_layer_with_gates_far_from_zero(T, dtype):
     out = routed.experts_forward(x.to(DEV), ids.to(DEV), w.to(DEV), on_gpu(up, group), on_gpu(down, group, False))
     assert bool(out.isfinite().all())
     assert_close(out, want, tol, t)
+
+
+# ------------------------------------------------------------------------------------------- results of pairs without an expert
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,k,D,type_", [(1, 1, 8, "f32"), (40, 3, 72, "bf16"), (300, 8, 264, "f16"), (7, 13, 1032, "f32"), (5, 64, 24, "bf16")])
+@pytest.mark.parametrize("kind", ["first", "last", "one", "none"])
+def test_sums_of_rows_with_few_results(T, k, D, type_, kind):
+    """The kernel reads zeros in the place of results that do not count; these are NaN here, so that one that got into a sum would show."""
+    t = TYPES[type_]
+    gen = torch.Generator().manual_seed(T + k)
+    y, w = torch.randn((T * k, D), generator=gen).to(t), torch.randn((T, k), generator=gen)
+    ids = torch.randint(0, 5, (T, k), generator=gen, dtype=torch.int32)
+    keep = dict(first=torch.arange(k) == 0, last=torch.arange(k) == k - 1, one=torch.arange(k) == torch.randint(0, k, (T, 1), generator=gen), none=torch.zeros(k, dtype=torch.bool))[kind]
+    ids = torch.where(keep.expand(T, k), ids, torch.tensor(-1 if T % 2 else 5, dtype=torch.int32))
+    ids[T // 2] = 7                                                        # a row of none among the others
+    there = ((ids >= 0) & (ids < 5)).numpy()
+    terms = np64(w)[..., None] * np64(y).reshape(T, k, D) * there[..., None]
+    y[~there.reshape(-1)] = math.nan
+    out = routed.route_combine(y.to(DEV), ids.to(DEV), w.to(DEV), n_experts=5)
+    assert_close(out, terms.sum(1), U * np.abs(terms).sum(1), t)           # one term a row: its product is the one rounding
+    assert bool((out[T // 2] == 0).all())
