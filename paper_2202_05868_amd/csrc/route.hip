@@ -285,7 +285,7 @@ __device__ __forceinline__ bool choose(const TopkParams &p, const float (&key)[V
         sort_falling(x);
     }
     if (p.n_groups > p.top_groups) {
-        float mine, before = INFINITY, wide = 2 * bound + widest * 0x1p-22f;      // of the sums of two keys, which are rounded
+        float mine, before = INFINITY, wide = bound + widest * 0x1p-23f;      // of half the sums of two keys (a sum may be beyond the type), which are rounded
         int group = sub;
         if (by_lanes) {
             int best = x[0], second = V > 1 ? x[V > 1] : kClosed;
@@ -296,8 +296,8 @@ __device__ __forceinline__ bool choose(const TopkParams &p, const float (&key)[V
             if (p.lanes_a_group >= 2) merge((int)from_lane<0xB1>((uint32_t)best), (int)from_lane<0xB1>((uint32_t)second));
             if (p.lanes_a_group >= 4) merge((int)from_lane<0x4E>((uint32_t)best), (int)from_lane<0x4E>((uint32_t)second));
             if (p.lanes_a_group >= 8) merge((int)from_lane<0x141>((uint32_t)best), (int)from_lane<0x141>((uint32_t)second));
-            mine = best <= kClosed ? -INFINITY : of_ordered(best & -V) + (second <= kClosed ? 0.f : of_ordered(second & -V));
-            wide += widest * (2 * V * 0x1p-23f);
+            mine = best <= kClosed ? -INFINITY : 0.5f * of_ordered(best & -V) + (second <= kClosed ? 0.f : 0.5f * of_ordered(second & -V));
+            wide += widest * (V * 0x1p-23f);
             group = sub / p.lanes_a_group;
         } else {
             // by way of LDS (one more place after every 16, or lanes meet in the same bank), a group a lane
@@ -314,7 +314,7 @@ __device__ __forceinline__ bool choose(const TopkParams &p, const float (&key)[V
                     best = fmaxf(best, y);
                 }
             }
-            mine = second > -INFINITY ? best + second : best;
+            mine = 0.5f * best + (second > -INFINITY ? 0.5f * second : 0.f);
         }
         if constexpr (LP == 16) {
             // By how many are before it; of equal ones that would be chosen together too many are, and the row is in doubt.
@@ -461,13 +461,13 @@ __global__ void __launch_bounds__(kRouteThreads) route_topk_kernel(const TopkPar
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const float s = l[v] > -INFINITY ? key[v] + bias[v] : -INFINITY;
-            key[v] = s > -INFINITY ? s : -INFINITY;                        // (NaN closes)
+            key[v] = s > -INFINITY ? fminf(s, FLT_MAX) : -INFINITY;        // (NaN closes)
             widest = fmaxf(widest, fabsf(s) < INFINITY ? fabsf(s) : 0.f);
         }
         widest = row_max<LP>(widest);
         // A sigmoid is off by 8 half steps at 1 at most (exponential, sum, reciprocal, product), a softmax by those of the largest one, 1 / total, and what
         // V + 6 additions in a row leave in its sum, and the sum with the bias by half a step of itself; two of them differ by as much again.
-        unsure = choose<LP, V>(p, key, l, row_lds, sub, my_id, 0x1p-24f * ((p.sigmoid ? 16.f : (36 + 2 * V) * one_of_total) + 4 * widest), widest, false);
+        unsure = choose<LP, V>(p, key, l, row_lds, sub, my_id, 0x1p-24f * (p.sigmoid ? 16.f : (36 + 2 * V) * one_of_total) + 0x1p-22f * widest, widest, false);
     } else {
         // numbers of 16 bits leave the lowest bits of 32 free, and nothing is lost
         unsure = choose<LP, V>(p, l, l, row_lds, sub, my_id, 0.f, 0.f, TY != VBR_F32);

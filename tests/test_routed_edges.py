@@ -6,7 +6,9 @@ import pytest
 import torch
 
 from paper_2202_05868_amd import routed
-from test_routed import DEV, TYPES, U, assert_close, gated, layer_of, matrices, np64, product
+from test_routed import DEV, TYPES, U, assert_close, choice, gated, layer_of, matrices, np64, product
+
+LOWEST = torch.finfo(torch.float32).min
 
 
 # ------------------------------------------------------------------------------------------- gates
@@ -83,6 +85,42 @@ def test_a_layer_with_gates_far_from_zero(T, dtype):
     out = routed.experts_forward(x.to(DEV), ids.to(DEV), w.to(DEV), on_gpu(up, group), on_gpu(down, group, False))
     assert bool(out.isfinite().all())
     assert_close(out, want, tol, t)
+
+
+# ------------------------------------------------------------------------------------------- biases of the lowest number
+def lowest_biases(kind, E, groups):
+    size = E // groups
+    b = torch.full((E,), LOWEST)
+    if kind == "one open":                     # and the others of its group closed for good
+        b[size: 2 * size] = -math.inf
+        b[size + 1 if size > 1 else size] = 0.25
+    if kind == "few":
+        b = torch.full((E,), -math.inf)
+        b[::3] = LOWEST
+        b[1] = 0.5
+    if kind == "high":                         # sums of two are beyond fp32
+        b = 3e38 - 1e37 * torch.arange(E, dtype=torch.float32).flip(0) % 7e37
+    if kind == "infinite":
+        b = torch.full((E,), 0.1)
+        b[size - 1::size] = math.inf
+        b[E // 2] = torch.finfo(torch.float32).max
+    return b
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["all", "one open", "few", "high", "infinite"])
+@pytest.mark.parametrize("T", [5, 2048])
+@pytest.mark.parametrize("E,groups,top_groups,k", [(32, 16, 3, 4), (16, 8, 2, 3), (60, 4, 2, 20), (256, 8, 3, 8), (12, 12, 5, 4), (64, 32, 4, 7), (576, 64, 5, 6)])
+def test_groups_of_biases_at_the_ends_of_the_range(kind, T, E, groups, top_groups, k):
+    gen = torch.Generator().manual_seed(E)
+    l = torch.randn((T, E), generator=gen)
+    b = lowest_biases(kind, E, groups)
+    for score in ("sigmoid", "softmax"):
+        ids, weights = routed.route_topk(l.to(DEV), k, score=score, bias=b.to(DEV), n_groups=groups, top_groups=top_groups, renormalise=False)
+        some = slice(0, 40)
+        want, w, _ = choice(np64(l)[some], k, score, np64(b), groups, top_groups, False, 1.0)
+        assert np.array_equal(ids[some].cpu().numpy(), want)
+        assert np.allclose(np64(weights)[some], w, rtol=2.0 ** -17, atol=0)     # scores of |l| < 8 in fp32: 2 * 8 + 80 roundings, and more
 
 
 # ------------------------------------------------------------------------------------------- results of pairs without an expert
