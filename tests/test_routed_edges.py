@@ -123,6 +123,60 @@ def test_groups_of_biases_at_the_ends_of_the_range(kind, T, E, groups, top_group
         assert np.allclose(np64(weights)[some], w, rtol=2.0 ** -17, atol=0)     # scores of |l| < 8 in fp32: 2 * 8 + 80 roundings, and more
 
 
+# ------------------------------------------------------------------------------------------- sums near each other
+def choice_of_all(l, k, score, bias, groups, top_groups):
+    """ids [T, k] of all rows at once; -inf closes."""
+    T, E = l.shape
+    closed = l == -np.inf
+    if score == "softmax":
+        most = l.max(1, keepdims=True)
+        e = np.exp(l - np.where(most == -np.inf, 0, most))
+        s = e / np.maximum(e.sum(1, keepdims=True), 1e-300)
+    else:
+        s = np.where(closed, 0, 1 / (1 + np.exp(-l)))
+    key = s + (0 if bias is None else bias)
+    out = closed | (key == -np.inf)
+    if groups > 1:
+        by = -np.sort(-np.where(out, -np.inf, key).reshape(T, groups, -1), 2)[:, :, :2]
+        total = by[:, :, 0] + np.where(by[:, :, -1] == -np.inf, 0, by[:, :, -1]) * (by.shape[2] > 1)
+        stays = np.argsort(-total, 1, kind="stable")[:, :top_groups]
+        mask = np.zeros((T, groups), bool)
+        np.put_along_axis(mask, stays, True, 1)
+        out |= ~np.repeat(mask, E // groups, 1)
+    order = l if bias is None else key
+    want = np.argsort(-np.where(out, -np.inf, order), 1, kind="stable")[:, :k]
+    return np.where(np.take_along_axis(out, want, 1), -1, want)
+
+
+def near_scores(seed, T, E):
+    """Rows of scores that 32 bits tell apart, and rows of scores that they do not, once a bias is added; some closed."""
+    gen = torch.Generator().manual_seed(seed)
+    l = 1.5 * torch.randn((T, E), generator=gen)
+    near = torch.rand((T, 1), generator=gen) < 0.5
+    l = torch.where(near, l[:, :1] * (1 + 1e-7 * torch.randint(-3, 4, (T, E), generator=gen)), l)
+    l = torch.where(torch.rand((T, E), generator=gen) < 0.05, torch.tensor(-math.inf), l)
+    l[T // 3: T // 3 + 3] = -math.inf
+    return l
+
+
+# on both sides of where a row has 64 lanes, and of more experts, places and groups than 16 lanes take
+@pytest.mark.gpu
+@pytest.mark.parametrize("far", [None, -1e4, -1e9, LOWEST, -math.inf, 100.0])
+@pytest.mark.parametrize("T,E,k,score,step,groups,top_groups", [
+    (700, 256, 8, "sigmoid", 2.0 ** -24, 8, 4), (2047, 256, 8, "softmax", 2.0 ** -26, 8, 3), (2048, 256, 8, "sigmoid", 2.0 ** -24, 8, 4), (2048, 96, 6, "softmax", 2.0 ** -26, 12, 5),
+    (2500, 100, 5, "sigmoid", 2.0 ** -24, 5, 2), (900, 512, 8, "sigmoid", 2.0 ** -24, 16, 4), (900, 1024, 8, "softmax", 2.0 ** -28, 32, 5), (800, 128, 33, "sigmoid", 2.0 ** -24, 1, 1),
+    (800, 1024, 12, "sigmoid", 2.0 ** -24, 1, 1), (700, 160, 6, "softmax", 2.0 ** -26, 32, 7), (700, 300, 9, "sigmoid", 2.0 ** -24, 20, 6), (600, 64, 4, "softmax", 2.0 ** -24, 32, 3)])
+def test_choices_of_sums_near_each_other(T, E, k, score, step, groups, top_groups, far):
+    l = near_scores(E + T, T, E)
+    gen = torch.Generator().manual_seed(E)
+    bias = step * torch.randn(E, generator=gen)
+    if far is not None:                                    # a third of the experts
+        bias = torch.where(torch.rand(E, generator=gen) < 0.33, torch.tensor(far), bias)
+    want = choice_of_all(np64(l), k, score, np64(bias), groups, top_groups)
+    ids, _ = routed.route_topk(l.to(DEV), k, score=score, bias=bias.to(DEV), n_groups=groups, top_groups=top_groups)
+    assert np.array_equal(ids.cpu().numpy(), want)
+
+
 # ------------------------------------------------------------------------------------------- results of pairs without an expert
 @pytest.mark.gpu
 @pytest.mark.parametrize("T,k,D,type_", [(1, 1, 8, "f32"), (40, 3, 72, "bf16"), (300, 8, 264, "f16"), (7, 13, 1032, "f32"), (5, 64, 24, "bf16")])
