@@ -263,12 +263,14 @@ __device__ __forceinline__ void sort_falling(int (&x)[V])
 }
 
 // The same in 32 bits.  Keys are whole numbers in the order of the numbers, with an expert's place in its lane in the lowest bits, lower places first: a lane sorts
-// its keys once, and a choice is the largest of the lanes' first ones.  The result says whether any difference that decides may be of the other sign.  `bound`
-// is what the difference of two keys may be off by, and a key without its lowest bits is lower by up to V steps: of two that differ the higher one is
-// higher by at least the difference less V steps of the lower.  Raw scores are what they are: those that differ without their lowest bits are in order.
-// widest: the largest of the row's finite keys in magnitude.  exact: the lowest bits were zero, and there is nothing to say.
+// its keys once, and a choice is the largest of the lanes' first ones.  The result says whether any difference that decides may be of the other sign.  A key is
+// off by `bound` at most, and by kOff of its own size, and one without its lowest bits is lower by up to V steps: of two that differ the higher one is
+// higher by at least the difference less what both are off by and V steps of the lower.  What a key can be at most rises with it, so that one further
+// down than the next cannot come before the last chosen one if the next cannot.  Raw scores are what they are: those that differ without their lowest bits are in order.
+// exact: the lowest bits were zero, and there is nothing to say.
+constexpr float kOff = 0x1p-23f;
 template <int LP, int V>
-__device__ __forceinline__ bool choose(const TopkParams &p, const float (&key)[V], const float (&l)[V], float *lds, int sub, int &my_id, float bound, float widest, bool exact)
+__device__ __forceinline__ bool choose(const TopkParams &p, const float (&key)[V], const float (&l)[V], float *lds, int sub, int &my_id, float bound, bool exact)
 {
     bool unsure = false;              // (the same in every lane of the row)
     uint64_t chosen = ~0ull;          // groups
@@ -285,7 +287,7 @@ __device__ __forceinline__ bool choose(const TopkParams &p, const float (&key)[V
         sort_falling(x);
     }
     if (p.n_groups > p.top_groups) {
-        float mine, before = INFINITY, wide = bound + widest * 0x1p-23f;      // of half the sums of two keys (a sum may be beyond the type), which are rounded
+        float mine, size, lower = 0.f;                    // half the sum of a group's two best keys (a sum may be beyond the type), of their sizes, and what it may be too low by
         int group = sub;
         if (by_lanes) {
             int best = x[0], second = V > 1 ? x[V > 1] : kClosed;
@@ -296,8 +298,10 @@ __device__ __forceinline__ bool choose(const TopkParams &p, const float (&key)[V
             if (p.lanes_a_group >= 2) merge((int)from_lane<0xB1>((uint32_t)best), (int)from_lane<0xB1>((uint32_t)second));
             if (p.lanes_a_group >= 4) merge((int)from_lane<0x4E>((uint32_t)best), (int)from_lane<0x4E>((uint32_t)second));
             if (p.lanes_a_group >= 8) merge((int)from_lane<0x141>((uint32_t)best), (int)from_lane<0x141>((uint32_t)second));
-            mine = best <= kClosed ? -INFINITY : 0.5f * of_ordered(best & -V) + (second <= kClosed ? 0.f : 0.5f * of_ordered(second & -V));
-            wide += widest * (V * 0x1p-23f);
+            const float a = best <= kClosed ? -INFINITY : 0.5f * of_ordered(best & -V), b = second <= kClosed ? 0.f : 0.5f * of_ordered(second & -V);
+            mine = a + b;
+            size = fabsf(a) + fabsf(b);
+            lower = size * (V * 0x1p-23f);
             group = sub / p.lanes_a_group;
         } else {
             // by way of LDS (one more place after every 16, or lanes meet in the same bank), a group a lane
@@ -314,8 +318,11 @@ __device__ __forceinline__ bool choose(const TopkParams &p, const float (&key)[V
                     best = fmaxf(best, y);
                 }
             }
-            mine = 0.5f * best + (second > -INFINITY ? 0.5f * second : 0.f);
+            const float a = 0.5f * best, b = second > -INFINITY ? 0.5f * second : 0.f;
+            mine = a + b;
+            size = fabsf(a) + fabsf(b);
         }
+        const float sum = mine, off = bound + 2 * kOff * size;               // (and rounded itself)
         if constexpr (LP == 16) {
             // By how many are before it; of equal ones that would be chosen together too many are, and the row is in doubt.
             int ahead = 0;
@@ -323,21 +330,21 @@ __device__ __forceinline__ bool choose(const TopkParams &p, const float (&key)[V
             const int wanted = p.top_groups * (by_lanes ? p.lanes_a_group : 1);
             stays = ahead < wanted && mine > -INFINITY;
             const uint32_t in = (uint32_t)(__ballot(stays) >> (threadIdx.x & 48)) & 0xFFFFu;
-            const float last = -row_max<LP>(stays ? -mine : -INFINITY), next = row_max<LP>(stays ? -INFINITY : mine);
-            unsure = __popc(in) > wanted || (next > -INFINITY && last - next <= wide);
+            unsure = __popc(in) > wanted;
             chosen = in;
         } else {
             chosen = 0;
-            for (int i = 0; i <= p.top_groups; ++i) {
+            for (int i = 0; i < p.top_groups; ++i) {
                 const float top = row_max<LP>(mine);
                 const int at = row_min<LP>(mine == top && top > -INFINITY ? group : INT_MAX);
-                if (i == p.top_groups) unsure = top > -INFINITY && before - top <= wide;
-                else if (at != INT_MAX) chosen |= 1ull << at;
+                if (at != INT_MAX) chosen |= 1ull << at;
                 if (group == at) mine = -INFINITY;
-                before = top;
             }
             stays = chosen >> group & 1;
         }
+        // the least that one that stays can be, and the most that one that does not
+        const float least = -row_max<LP>(stays ? off - sum : -INFINITY), most = row_max<LP>(!stays && sum > -INFINITY ? sum + off + lower : -INFINITY);
+        unsure |= least <= most;
     }
     if (by_raw) {
         pack(l);
@@ -354,14 +361,14 @@ __device__ __forceinline__ bool choose(const TopkParams &p, const float (&key)[V
         for (int v = 0; v < V; ++v) x[v] = chosen >> ((uint32_t)(sub * V + V - 1 - (x[v] & (V - 1))) * p.group_factor >> 20) & 1 ? x[v] : kClosed;
         sort_falling(x);
     }
-    const float by = by_raw ? 0.f : bound, lost = by_raw ? 0.f : V * 0x1p-23f;
+    const float by = by_raw ? 0.f : 2 * bound, off = by_raw ? 0.f : kOff, lost = by_raw ? 0.f : kOff + V * 0x1p-23f;
     float before = INFINITY;
     for (int j = 0; j < p.top_k + (exact ? 0 : 1); ++j) {
         const int first = x[0] & -V, most = row_max_int<LP>(first), mine = sub * V + V - 1 - (x[0] & (V - 1));      // (places count among equal keys only)
         const int at = row_min<LP>(first == most && most > kClosed ? mine : INT_MAX);
         if (!exact) {
             const float now = of_ordered(most);
-            unsure |= j > 0 && most > kClosed && before - now <= by + fabsf(now) * lost;
+            unsure |= j > 0 && most > kClosed && before - now <= by + fabsf(before) * off + fabsf(now) * lost;
             before = now;
         }
         if (j < p.top_k && sub == j) my_id = at == INT_MAX ? -1 : at;
@@ -449,7 +456,6 @@ __global__ void __launch_bounds__(kRouteThreads) route_topk_kernel(const TopkPar
 #pragma unroll
             for (int v = 0; v < V; ++v) bias[v] = 0.f;
         }
-        float widest = 0.f;
         const float one_of_total = 1.f / total;
         if (p.sigmoid) {
 #pragma unroll
@@ -462,15 +468,13 @@ __global__ void __launch_bounds__(kRouteThreads) route_topk_kernel(const TopkPar
         for (int v = 0; v < V; ++v) {
             const float s = l[v] > -INFINITY ? key[v] + bias[v] : -INFINITY;
             key[v] = s > -INFINITY ? fminf(s, FLT_MAX) : -INFINITY;        // (NaN closes)
-            widest = fmaxf(widest, fabsf(s) < INFINITY ? fabsf(s) : 0.f);
         }
-        widest = row_max<LP>(widest);
         // A sigmoid is off by 8 half steps at 1 at most (exponential, sum, reciprocal, product), a softmax by those of the largest one, 1 / total, and what
-        // V + 6 additions in a row leave in its sum, and the sum with the bias by half a step of itself; two of them differ by as much again.
-        unsure = choose<LP, V>(p, key, l, row_lds, sub, my_id, 0x1p-24f * (p.sigmoid ? 16.f : (36 + 2 * V) * one_of_total) + 0x1p-22f * widest, widest, false);
+        // V + 6 additions in a row leave in its sum; the sum with the bias by half a step of itself.
+        unsure = choose<LP, V>(p, key, l, row_lds, sub, my_id, 0x1p-24f * (p.sigmoid ? 8.f : (18 + V) * one_of_total), false);
     } else {
         // numbers of 16 bits leave the lowest bits of 32 free, and nothing is lost
-        unsure = choose<LP, V>(p, l, l, row_lds, sub, my_id, 0.f, 0.f, TY != VBR_F32);
+        unsure = choose<LP, V>(p, l, l, row_lds, sub, my_id, 0.f, TY != VBR_F32);
     }
     // rows in doubt, one after the other, by the whole wave
     for (uint64_t doubt = __ballot(unsure); doubt != 0;) {
