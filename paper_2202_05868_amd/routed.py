@@ -11,6 +11,10 @@ current stream of the operands' device, and there is no fallback.
 
 or step by step: ``plan = route_plan(ids, n_experts)``, ``h = up.mm_routed(x, plan)``, ``y = down.mm_routed(h, plan)``,
 ``out = route_combine(y, ids, weights)``.
+
+Autograd does not see any of it: where gradients are recorded, the calls forward refuse operands that require one instead of giving results that are
+cut off from them.  ``route_topk_grad`` and ``route_combine_grad`` are the router's and the sum's gradients, to be called with gradients
+off (inside a ``torch.autograd.Function``, for instance); matrices in 4 bits are frozen, and their products pass none on to ``x``.
 """
 from __future__ import annotations
 
@@ -52,6 +56,11 @@ def _rows(what, name, t, n_rows, n_cols, types):
     return stride[0]
 
 
+def _cut_off(what):
+    if torch.is_grad_enabled():
+        raise ValueError("%s: an operand requires a gradient, which autograd would not get through this call: detach it, or call under torch.no_grad()" % what)
+
+
 def _dense(what, name, t, shape, dtype):
     if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
         raise ValueError("%s: %s must be a contiguous %s tensor of shape %s" % (what, name, dtype, tuple(shape)))
@@ -78,6 +87,8 @@ def route_topk(logits, k, *, score="softmax", bias=None, n_groups=1, top_groups=
     """The ``k`` experts of every row of ``logits`` [T, E] (float32, bfloat16 or float16; row stride free) and their weights: int32 and float32
     [T, k], allocated here unless given.  ``bias``: float32 [E], added to the scores for the choice alone."""
     what = "route_topk"
+    if logits.requires_grad:
+        _cut_off(what)
     ld = _rows(what, "logits", logits, None, None, _TYPES)
     n_rows, n_experts = logits.shape
     device = logits.get_device()
@@ -163,6 +174,8 @@ def route_combine(y, ids, weights, out=None, *, out_dtype=None, n_experts=_ANY):
     """out[t] = sum over j of weights[t, j] * y[t k + j], in ``out_dtype`` (y's, if not given).  Pairs whose id is negative, or not below
     ``n_experts``, are left out."""
     what = "route_combine"
+    if y.requires_grad or weights.requires_grad:
+        _cut_off(what)
     n_rows, k, n_cols, ldy, device = _sum_operands(what, y, ids, weights)
     if out_dtype is not None and (out_dtype not in _TYPES or (out is not None and out.dtype is not out_dtype)):
         raise ValueError("%s: out_dtype must be float32, bfloat16 or float16, and out's" % what)
@@ -266,6 +279,8 @@ class Q4:
         return self
 
     def _operands(self, what, x, n_out, y, y_dtype):
+        if x.requires_grad:
+            _cut_off(what)
         ldx = _rows(what, "x", x, None, self.n_cols, (self.dtype,))
         if y is None:
             if y_dtype is not None and y_dtype is not self.dtype and y_dtype is not torch.float32:
@@ -310,6 +325,8 @@ def experts_forward(x, ids, weights, up, down, out=None):
     if not up.gated or up.n_out != down.n_cols or up.n_mats != down.n_mats or down.gated or up.dtype is not down.dtype:
         raise ValueError("experts_forward: up must be gated, and down take what it gives, of as many experts and the same type")
     what = "experts_forward"
+    if x.requires_grad or weights.requires_grad:
+        _cut_off(what)
     if ids.dim() != 2:
         raise ValueError("%s: ids must be of shape (T, k)" % what)
     n_rows, k = ids.shape

@@ -5,8 +5,8 @@ import numpy as np
 import pytest
 import torch
 
-from paper_2202_05868_amd import routed
-from test_routed import DEV, TYPES, U, assert_close, choice, gated, layer_of, matrices, np64, product
+from paper_2202_05868_amd import binding, routed
+from test_routed import DEV, TYPES, U, assert_close, choice, choice_grad, gated, layer_of, matrices, np64, product
 
 LOWEST = torch.finfo(torch.float32).min
 
@@ -196,3 +196,53 @@ def test_sums_of_rows_with_few_results(T, k, D, type_, kind):
     out = routed.route_combine(y.to(DEV), ids.to(DEV), w.to(DEV), n_experts=5)
     assert_close(out, terms.sum(1), U * np.abs(terms).sum(1), t)           # one term a row: its product is the one rounding
     assert bool((out[T // 2] == 0).all())
+
+
+# ------------------------------------------------------------------------------------------- gradients that would be lost
+def test_operands_that_require_a_gradient_are_refused():
+    l, x, y = torch.zeros((4, 12)), torch.zeros((4, 128), dtype=torch.float16), torch.zeros((8, 16))
+    ids, w = torch.zeros((4, 2), dtype=torch.int32), torch.zeros((4, 2))
+    up = routed.Q4(torch.zeros((3, 8, 64), dtype=torch.uint8), torch.zeros((3, 8, 2), dtype=torch.float16), group=64, gated=True)
+    down = routed.Q4(torch.zeros((3, 8, 16), dtype=torch.uint8), torch.zeros((3, 8, 1), dtype=torch.float16), group=32)
+    up.n_out = down.n_cols                                                  # (matrices that no call gets as far as multiplying)
+    plan = routed.RoutePlan(torch.zeros(64, dtype=torch.int32), 4, 2, 3)
+    bias = torch.zeros(12, requires_grad=True)
+    calls = [(l, lambda l: routed.route_topk(l, 2)), (y, lambda y: routed.route_combine(y, ids, w)), (w, lambda w: routed.route_combine(y, ids, w)),
+             (x, lambda x: up.mm(x)), (x, lambda x: up.mm_routed(x, plan)), (x, lambda x: routed.experts_forward(x, ids, w, up, down)),
+             (w, lambda w: routed.experts_forward(x, ids, w, up, down))]
+    for t, call in calls:
+        with pytest.raises(ValueError, match="requires a gradient"):
+            call(t.clone().requires_grad_())
+        with torch.no_grad(), pytest.raises((ValueError, binding.VbrError)) as e:        # gets as far as the GPU that is not there
+            call(t.clone().requires_grad_())
+        assert "gradient" not in str(e.value)
+    with pytest.raises(ValueError, match="on the GPU"):                     # no gradient reaches a bias
+        routed.route_topk(l, 2, bias=bias)
+    with pytest.raises(ValueError, match="on the GPU"):                     # nor is one lost of a gradient's own operands
+        routed.route_topk_grad(l.requires_grad_(), ids, w)
+
+
+@pytest.mark.gpu
+def test_a_router_under_autograd():
+    """The router's choice and its gradient inside a function of autograd's."""
+    class Weights(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, l):
+            ids, w = routed.route_topk(l, 3, scale=1.5)
+            ctx.save_for_backward(l, ids)
+            ctx.mark_non_differentiable(ids)
+            return w, ids
+
+        @staticmethod
+        def backward(ctx, dw, _):
+            l, ids = ctx.saved_tensors
+            return routed.route_topk_grad(l, ids, dw.contiguous(), scale=1.5)
+
+    gen = torch.Generator().manual_seed(1)
+    l0, dw = torch.randn((30, 20), generator=gen), torch.randn((30, 3), generator=gen)
+    l = l0.to(DEV).requires_grad_()
+    w, ids = Weights.apply(l)
+    (w * dw.to(DEV)).sum().backward()
+    want = choice_grad(np64(l0), ids.cpu().numpy().astype(np.int64), np64(dw), "softmax", True, 1.5)
+    # every term of the gradient is at most 1.5 |dw|
+    assert np.all(np.abs(np64(l.grad) - want) <= U * 400 * 1.5 * np.abs(np64(dw)).sum(1, keepdims=True))
