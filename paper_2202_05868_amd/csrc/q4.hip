@@ -14,7 +14,6 @@
 
 #include "route.h"
 #include "vbr_device.h"
-#include "vbr_host.h"
 
 // A tile is 16 rows (of one half, if gated) and 128 columns: 1 KiB of codes, 16 bytes a lane.  Lane 16 q + n has row n; its word i has the
 // columns 32 i + 8 q .. + 7, in the order that the rotations take them apart.  Tiles of a row follow each other; with a gate the tiles of 16
@@ -815,18 +814,18 @@ __global__ void __launch_bounds__(256, 2) q4_many_kernel(const MmParams p)
 using MmKernel = void (*)(MmParams);
 struct Variant {
     MmKernel kernel;
-    int32_t rows, tile_rows, threads, lds;             // of a workgroup
+    int32_t tile_rows, threads, lds;                   // of a workgroup
 };
 template <int DT, int CH, bool ZEROS, int NT, int AHEAD_W, int AHEAD_X, int THREADS>
 Variant split_variant(int waves)
 {
-    return {q4_split_kernel<DT, CH, ZEROS, NT, AHEAD_W, AHEAD_X, THREADS>, 16, NT, 64 * waves, waves * NT * 16 * kSumRow * 4};
+    return {q4_split_kernel<DT, CH, ZEROS, NT, AHEAD_W, AHEAD_X, THREADS>, NT, 64 * waves, waves * NT * 16 * kSumRow * 4};
 }
 template <int DT, int CH, bool ZEROS, int MT>
 Variant mid_variant(int waves)
 {
     const int x = waves * 32 * MT * 256, halves = waves / 2 * MT * 2 * 4096, out = MT * 2 * 4096 + waves * 32 * kSumRow32 * 4;
-    return {q4_mid_kernel<DT, CH, ZEROS, MT>, 32 * MT, 4, 64 * waves, std::max(x, std::max(halves, out))};
+    return {q4_mid_kernel<DT, CH, ZEROS, MT>, 4, 64 * waves, std::max(x, std::max(halves, out))};
 }
 
 // The variant for `rows` rows of a tile of rows (16, 32 or 64): nt rows of tiles a workgroup (16 of more than 16 rows: the kernel for many workgroups).
@@ -839,7 +838,7 @@ Variant mm_variant(const Choice &c)
     if (c.rows == 16)
         return c.nt == 1 ? split_variant<DT, CH, ZEROS, 1, 4, 2, 512>(c.waves) : c.nt == 2 ? split_variant<DT, CH, ZEROS, 2, 1, 1, 512>(c.waves) : split_variant<DT, CH, ZEROS, 4, 2, 2, 256>(c.waves);
     if (c.nt == 4) return c.rows == 32 ? mid_variant<DT, CH, ZEROS, 1>(c.waves) : mid_variant<DT, CH, ZEROS, 2>(c.waves);
-    return c.rows == 32 ? Variant{q4_many_kernel<DT, CH, ZEROS, 1>, 32, 16, 256, 0} : Variant{q4_many_kernel<DT, CH, ZEROS, 2>, 64, 16, 256, 0};
+    return c.rows == 32 ? Variant{q4_many_kernel<DT, CH, ZEROS, 1>, 16, 256, 0} : Variant{q4_many_kernel<DT, CH, ZEROS, 2>, 16, 256, 0};
 }
 template <int DT>
 Variant mm_variant(int32_t group, bool zeros, const Choice &c)
@@ -855,18 +854,6 @@ MmKernel sum_kernel(int32_t group, bool zeros)
     if (group == 32) return zeros ? q4_sum_kernel<DT, 1, true> : q4_sum_kernel<DT, 1, false>;
     if (group == 64) return zeros ? q4_sum_kernel<DT, 2, true> : q4_sum_kernel<DT, 2, false>;
     return zeros ? q4_sum_kernel<DT, 4, true> : q4_sum_kernel<DT, 4, false>;
-}
-
-bool aligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
-
-int launched()
-{
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) {
-        set_last_hip_error((int)e);
-        return VBR_EHIP;
-    }
-    return VBR_OK;
 }
 
 // What both products ask of their operands; n_rows of Y

@@ -1,11 +1,11 @@
-// The layout of a plan (route_plan), which the routed products read.
+// What route.hip and q4.hip share: limits, the layout of a plan (route_plan), which the routed products read, and their launches' ends.
 #pragma once
 
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
 
-#include "vbr_spmm.h"
+#include "vbr_host.h"
 
 namespace vbrk {
 
@@ -28,6 +28,18 @@ struct Divide {
     }
     __host__ __device__ uint32_t operator()(uint32_t i) const { return (uint32_t)((uint64_t)i * factor >> shift); }
 };
+
+inline bool aligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+
+inline int launched()                              // what became of the last launch
+{
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) {
+        set_last_hip_error((int)e);
+        return VBR_EHIP;
+    }
+    return VBR_OK;
+}
 
 // Byte offsets in a plan: int32 offsets [n_experts + 1] at 0, int32 order [n_pairs], PlanTile tiles [n_tiles],
 // int32 counts [n_parts][n_experts].

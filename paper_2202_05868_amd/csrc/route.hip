@@ -9,7 +9,6 @@
 
 #include "route.h"
 #include "vbr_device.h"
-#include "vbr_host.h"
 
 namespace vbrk {
 namespace {
@@ -899,16 +898,6 @@ __global__ void __launch_bounds__(kRouteThreads) route_combine_grad_kernel(const
     if (lane == 0) p.dweights[pair] = dot;
 }
 
-int launched()
-{
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) {
-        set_last_hip_error((int)e);
-        return VBR_EHIP;
-    }
-    return VBR_OK;
-}
-
 bool route_ok(const vbr_route_t *how)
 {
     if (!how || how->n_experts < 1 || how->n_experts > kMaxExperts || how->top_k < 1 || how->top_k > kMaxTopK || how->top_k > how->n_experts) return false;
@@ -919,7 +908,6 @@ bool route_ok(const vbr_route_t *how)
 }
 
 bool float_type(int32_t t) { return t == VBR_F16 || t == VBR_BF16 || t == VBR_F32; }
-bool aligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 int64_t up(int64_t x, int64_t q) { return (x + q - 1) / q * q; }
 
 // Lanes of a row: 16 where they can hold the experts and there are many rows, four a wave, 64 elsewhere: one row of them is done sooner.  In us with 16 and 64,
