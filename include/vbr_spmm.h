@@ -347,7 +347,7 @@ int route_combine_grad(const void *dout_dev, int64_t ldo, int32_t out_type, cons
  * Matrices in 4 bits: n_mats of n_rows x n_cols, W[n][k] = scale[n][k / group] * (code[n][k] - zero[n][k / group]), code and zero 0 .. 15.
  * n_cols % 32 == 0; group 32, 64 or a multiple of 128 (the last group of a row may be short).  dtype is the type of the scales and of the rows
  * they are multiplied with.  zeros = 0: the zero point is 8 everywhere.  gated: the first half of a matrix's rows gates the second,
- *   Y[r][n] = silu(x . W[n]) * (x . W[n + n_rows / 2]),  silu(u) = u / (1 + exp(-u)),
+ *   Y[r][n] = silu(x . W[n]) * (x . W[n + n_rows / 2]),  silu(u) = u / (1 + exp(-u)) for any finite u,
  * and Y has n_rows / 2 columns instead of n_rows.
  *   q4_upload   lays the matrices out in buf_dev (device memory of the current device, caller-allocated, q4_device_bytes bytes, 256-byte
  *               aligned) from device arrays, each without gaps:
@@ -374,7 +374,7 @@ void q4_free(q4_t *h);
  * A layer of experts in one call: out[row] = sum over its places of weights[pair] * (h[pair] D[expert]^T), h[pair] = gated product of X[row] with up's
  * matrix of the expert, D those of down: route_plan, q4_mm_routed twice and route_combine in turn.  up is gated and gives as many columns as down takes,
  * both have as many matrices and one dtype, and down's rows are a multiple of 8.  h is rounded to dtype, which the second product multiplies; its results stay in fp32 until
- * they are summed.  Operands as in those calls; work_dev: caller-allocated, experts_work_bytes bytes (0 for sizes that do not fit), 256-byte
+ * they are summed.  (With results in dtype a layer is off by 1.4 times what their own rounding costs.)  Operands as in those calls; work_dev: caller-allocated, experts_work_bytes bytes (0 for sizes that do not fit), 256-byte
  * aligned, of this call alone while it runs.  Few pairs, by the sizes alone, are multiplied as they stand, without a plan, and added up by the second product: the
  * sum of a row is then taken in another order.
  */

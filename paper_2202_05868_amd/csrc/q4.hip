@@ -592,7 +592,7 @@ __device__ __forceinline__ void store_32(const MmParams &p, int count, int token
 }
 
 // Few workgroups: the division of the work as above (192 rows times 4096 x 14336 in groups of 128: 38.7 us, 583 TFLOP/s; the waits for X and the unpacking, which
-// is done once for each 64 rows, stand between it and the 883 of the kernel below), with X through a part of LDS that each wave has for itself.  A wave's load takes 256 bytes of four rows
+// is done once for each 64 rows, stand between it and the 880 to 970 of the kernel below), with X through a part of LDS that each wave has for itself.  A wave's load takes 256 bytes of four rows
 // (the pieces of 32 bytes that the matrix units take are a part of a line each, and the rest is gone from the L1 before it is asked for).  The rows of a
 // step are read into registers at once and those of the next step fetched into their place.
 template <int DT, int CH, bool ZEROS, int MT>
@@ -720,9 +720,9 @@ __global__ void __launch_bounds__(512) q4_mid_kernel(const MmParams p)
 
 // Many workgroups: 32 MT rows of X times 16 rows of tiles, by four waves with four rows of tiles each.  X goes through LDS, which all waves read; W
 // comes straight into registers, as it was laid out, and is turned into numbers there.
-// Bound by the issue of instructions: beside each product of 32 x 32 x 16, which takes the place of about six vector instructions, stand for 64 rows 2.5 that make
-// numbers of W, 2 that apply a scale (groups of 128) and the loads from LDS.  2048 rows times 8192 x 8192 reach 883 TFLOP/s with zero points and 967
-// without; a product of bf16 with bf16 of the library reaches 1186 at 8192 x 8192 x 8192.
+// Bound by the issue of instructions: beside each product of 32 x 32 x 16, which takes the place of about six vector instructions, stand for 64 rows 3.5 that make
+// numbers of W (seven for two products), 2 that apply a scale (groups of 128) and the loads from LDS.  2048 rows times 8192 x 8192 reach 880 to 970 TFLOP/s with zero points
+// and 920 to 1005 without, from card to card; a product of bf16 with bf16 of the library reaches 1186 at 8192 x 8192 x 8192.
 template <int CTRL>
 __device__ __forceinline__ float add_lane(float x)
 {
@@ -1147,7 +1147,7 @@ extern "C" int experts_forward(const q4_t *up, const q4_t *down, const void *X_d
     if (!up->dev || !down->dev) return VBR_ESTATE;
     if (n_rows == 0) return VBR_OK;
     if (!ids_dev || !weights_dev || !out_dev || !work_dev || !aligned(work_dev, 256) || !aligned(ids_dev, 4) || !aligned(weights_dev, 4)) return VBR_EINVAL;
-    // (all that can be refused is, before anything is launched)
+    // (operands are refused before anything is launched; products of more workgroups than a launch can have, by themselves)
     if ((out_type != VBR_F16 && out_type != VBR_BF16 && out_type != VBR_F32) || ldo < down->n_rows || ldo % 8 != 0 || !aligned(out_dev, 16)) return VBR_EINVAL;
     const int64_t n_pairs = n_rows * top_k;
     const Work w = experts_work(up, down, n_pairs);

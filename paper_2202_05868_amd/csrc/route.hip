@@ -242,7 +242,7 @@ __device__ __forceinline__ int choose_exactly(const TopkParams &p, double (&key)
     return my_id;
 }
 
-// falling, by merging odd and even places: comparators that are known beforehand
+// falling, by Batcher's odd-even merge sort: comparators that are known beforehand
 template <int V>
 __device__ __forceinline__ void sort_falling(int (&x)[V])
 {
@@ -417,8 +417,8 @@ __device__ __forceinline__ int choose_row_exactly(const TopkParams &p, int64_t r
 
 // LP lanes a row, V experts a lane.  What decides between sums of scores and biases are differences that 32 bits may not tell: they are made in 32 bits, with a
 // bound for what they are off by, and where a difference is within it, in 64 bits.  Raw scores are compared as they are: the score rises with them.
-// Bound by the issue of vector instructions, some 1700 for four rows of 256 experts, most of them the sorting of a lane's keys and the choice itself: 16384 rows, 8
-// of 256 in 4 of 8 groups take 16 us, of which the rows in doubt are about 4; 8192 rows, 8 of 128 by raw scores 4.6.
+// 16384 rows, 8 of 256 in 4 of 8 groups, take 15.3 us: 8.5 are the issue of 1259 vector instructions for four rows, most of them the sorting of a lane's keys and the
+// choice itself, 2.5 the launch, and the rows in doubt end about 4 after the others; 8192 rows, 8 of 128 by raw scores, 4.5.
 template <int TY, int LP, int V>
 __global__ void __launch_bounds__(kRouteThreads) route_topk_kernel(const TopkParams p)
 {
