@@ -143,7 +143,7 @@ __device__ __forceinline__ float of_ordered(int i) { return number((uint32_t)(i 
 
 template <int LP>
 __device__ __forceinline__ int row_max_int(int x) { return (int)over_lanes<LP>((uint32_t)x, [](uint32_t a, uint32_t b) { return (uint32_t)((int)a > (int)b ? (int)a : (int)b); }); }
-constexpr int kClosed = (int)0x807FFFFF, kLargest = 0x7F7FFFFF;      // of -inf, and no number is as low; of FLT_MAX
+constexpr int kClosed = (int)0x807FFFFF;             // of -inf, and no number is as low
 
 // The choice among the keys, V a lane of the wave, in 64 bits: lane j gets the j-th expert, -1 without one.  Of equal keys the lower index wins.
 template <int V>
@@ -266,7 +266,8 @@ __device__ __forceinline__ void sort_falling(int (&x)[V])
 // off by `bound` at most, and by kOff of its own size, and one without its lowest bits is lower by up to V steps: of two that differ the higher one is
 // higher by at least the difference less what both are off by and V steps of the lower.  What a key can be at most rises with it, so that one further
 // down than the next cannot come before the last chosen one if the next cannot.  Raw scores are what they are: those that differ without their lowest bits are in order.
-// exact: the lowest bits were zero, and there is nothing to say.
+// exact: the lowest bits were zero, and there is nothing to say.  Infinite keys (of biases) are all equal, and so are the sums of groups that have one; what an
+// infinity is compared with is in doubt, but for another one in the order of their places.
 constexpr float kOff = 0x1p-23f;
 template <int LP, int V>
 __device__ __forceinline__ bool choose(const TopkParams &p, const float (&key)[V], const float (&l)[V], float *lds, int sub, int &my_id, float bound, bool exact)
@@ -277,7 +278,7 @@ __device__ __forceinline__ bool choose(const TopkParams &p, const float (&key)[V
     int x[V];
     auto pack = [&](const float (&from)[V]) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) x[v] = (min(ordered(from[v]), kLargest) & -V) | (V - 1 - v);
+        for (int v = 0; v < V; ++v) x[v] = (ordered(from[v]) & -V) | (V - 1 - v);
     };
     const bool by_raw = p.bias == nullptr;                // the same order, and exact
     const bool by_lanes = p.lanes_a_group && !by_raw;
@@ -417,7 +418,7 @@ __device__ __forceinline__ int choose_row_exactly(const TopkParams &p, int64_t r
 
 // LP lanes a row, V experts a lane.  What decides between sums of scores and biases are differences that 32 bits may not tell: they are made in 32 bits, with a
 // bound for what they are off by, and where a difference is within it, in 64 bits.  Raw scores are compared as they are: the score rises with them.
-// 16384 rows, 8 of 256 in 4 of 8 groups, take 15.3 us: 8.5 are the issue of 1259 vector instructions for four rows, most of them the sorting of a lane's keys and the
+// 16384 rows, 8 of 256 in 4 of 8 groups, take 14.7 us: 8.2 are the issue of 1225 vector instructions for four rows, most of them the sorting of a lane's keys and the
 // choice itself, 2.5 the launch, and the rows in doubt end about 4 after the others; 8192 rows, 8 of 128 by raw scores, 4.5.
 template <int TY, int LP, int V>
 __global__ void __launch_bounds__(kRouteThreads) route_topk_kernel(const TopkParams p)
@@ -466,7 +467,7 @@ __global__ void __launch_bounds__(kRouteThreads) route_topk_kernel(const TopkPar
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const float s = l[v] > -INFINITY ? key[v] + bias[v] : -INFINITY;
-            key[v] = s > -INFINITY ? fminf(s, FLT_MAX) : -INFINITY;        // (NaN closes)
+            key[v] = s > -INFINITY ? s : -INFINITY;                        // (NaN closes)
         }
         // A sigmoid is off by 8 half steps at 1 at most (exponential, sum, reciprocal, product), a softmax by those of the largest one, 1 / total, and what
         // V + 6 additions in a row leave in its sum; the sum with the bias by half a step of itself.

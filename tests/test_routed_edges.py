@@ -123,6 +123,24 @@ def test_groups_of_biases_at_the_ends_of_the_range(kind, T, E, groups, top_group
         assert np.allclose(np64(weights)[some], w, rtol=2.0 ** -17, atol=0)     # scores of |l| < 8 in fp32: 2 * 8 + 80 roundings, and more
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [5, 2048])
+@pytest.mark.parametrize("E,groups,top_groups,k", [(32, 16, 3, 4), (60, 4, 1, 5), (60, 4, 2, 9), (256, 8, 3, 8), (256, 8, 1, 3), (12, 12, 5, 4), (64, 32, 4, 7), (576, 64, 5, 6)])
+@pytest.mark.parametrize("infinite", [1, 2, 4])
+def test_groups_with_infinite_biases_come_first(T, E, groups, top_groups, k, infinite):
+    """The other groups have two biases that are larger than half of the largest number, those with an infinite one have low ones beside it."""
+    size = E // groups
+    l = torch.randn((T, E), generator=torch.Generator().manual_seed(E))
+    b = 3e38 * (1 - 0.3 * torch.arange(E) / E)
+    for g in range(infinite):
+        at = (groups - 1 - 2 * g) % groups * size
+        b[at: at + size] = -1e30
+        b[at + size // 2] = math.inf
+    ids, _ = routed.route_topk(l.to(DEV), k, score="sigmoid", bias=b.to(DEV), n_groups=groups, top_groups=top_groups)
+    want, _, _ = choice(np64(l)[:40], k, "sigmoid", np64(b), groups, top_groups, True, 1.0)
+    assert np.array_equal(ids[:40].cpu().numpy(), want)
+
+
 # ------------------------------------------------------------------------------------------- sums near each other
 def choice_of_all(l, k, score, bias, groups, top_groups):
     """ids [T, k] of all rows at once; -inf closes."""
