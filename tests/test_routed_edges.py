@@ -264,3 +264,25 @@ def test_a_router_under_autograd():
     want = choice_grad(np64(l0), ids.cpu().numpy().astype(np.int64), np64(dw), "softmax", True, 1.5)
     # every term of the gradient is at most 1.5 |dw|
     assert np.all(np.abs(np64(l.grad) - want) <= U * 400 * 1.5 * np.abs(np64(dw)).sum(1, keepdims=True))
+
+
+# ------------------------------------------------------------------------------------------- small numbers
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,N,K,group,zeros,gate", [(1, 200, 288, 32, True, False), (13, 66, 1056, 128, False, False), (16, 12000, 160, 64, True, False), (48, 5456, 288, 128, True, True),
+                                                    (130, 16384, 64, 32, True, False), (300, 8192, 160, 64, False, False), (1024, 8200, 96, 128, True, False)])
+@pytest.mark.parametrize("what", ["x", "scales", "both"])
+def test_products_of_numbers_below_the_normal_ones(T, N, K, group, zeros, gate, what):
+    """fp16 has numbers below 2^-14 with fewer bits: they are multiplied and summed as they are, like all others, and nothing of them is lost."""
+    gen = torch.Generator().manual_seed(T + N)
+    codes, scales, z = matrices(gen, 1, N, K, group, torch.float16, zeros)
+    x = torch.randn((T, K), generator=gen)
+    if what != "x":
+        scales = (scales.float() * 2.0 ** -11).half()                      # 0.02 to 1e-5
+    if what != "scales":
+        x = x * 2.0 ** torch.randint(-20, -14, (T, 1), generator=gen)
+    x, q = x.half(), (codes, scales, z)
+    want, tol = product(np64(x), q, 0, group)
+    if gate:
+        want, tol = gated(want, tol)
+    y = on_gpu(q, group, gate).mm(x.to(DEV), y_dtype=torch.float32)
+    assert_close(y, want, tol + 2.0 ** -126, torch.float32)
